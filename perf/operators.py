@@ -193,7 +193,6 @@ def prepare(case, seed):
         if own:
             from paper_2508_06753_b200 import binding as b
             s.lora = b.LoraGroup(s.A, s.B, rank=s.rank, scale=s.scale)
-            s.ws = b.new_workspace(b.w2a8_lora_workspace_bytes(M, L))
             s.y = [torch.zeros_like(t) for t in s.base]
         return s
 
@@ -278,7 +277,7 @@ def run(s):
         return _plain_lora(s) if op == "lora" else _plain_heads(s)
     from paper_2508_06753_b200 import binding as b
     if op == "lora":
-        return b.w2a8_lora_grouped(s.x, s.adapter, s.lora, s.ws, base=s.base, y=s.y)
+        return b.w2a8_lora_grouped(s.x, s.adapter, s.lora, base=s.base, y=s.y)
     if op == "rope":
         return b.w2a8_rope(s.grp, s.pos, s.inv_freq, s.amplitude, interleaved=s.case["interleaved"])
     return b.w2a8_qk_norm_rope(s.grp, s.eps, s.pos, s.inv_freq, s.amplitude, interleaved=s.case["interleaved"])
