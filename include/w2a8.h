@@ -393,6 +393,108 @@ int w2a8_linear_grouped_host(const void *x_host, int M, int K, int count, const 
                              void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * w2a8_lora_grouped -- low-rank adapters of many requests beside `count`
+ * (1 .. 4) projections that share their activations: the bf16 part that
+ * fine-tuning adds to the frozen 2-bit matrices of w2a8_linear_grouped.
+ * (The paper has no counterpart.)  For token m with adapter a = adapter[m],
+ * r = rank[a], s = scale[a], and every matrix i:
+ *   h[j]       = sum_k x[m][k] * A[i][a][j][k]                    (j < r)
+ *   y[i][m][n] = base[i][m][n] + sum_{j < r} B[i][a][n][j] * (s * h[j])
+ * A token whose adapter[m] lies outside [0, adapters) has none: y = base, bit
+ * for bit.  Sums are held in fp32, s * h is not rounded below 24 bits for an
+ * fp32 result (16 bits for a bf16 one), and y is rounded once.  Values of A and
+ * B at ranks of r and more are not used, whatever they hold.
+ *   x_bf16   [M][K] bf16, row-major
+ *   adapter  [M] int32, in any order (4-byte alignment suffices)
+ *   rank     [adapters] int32, clamped to 0 .. rank_max, or NULL: rank_max for all
+ *   scale    [adapters] fp32, or NULL: 1
+ *   A, B     HOST arrays of `count` DEVICE pointers: [adapters][rank_max][K] and
+ *            [adapters][N[i]][rank_max] bf16, row-major
+ *   base, y  HOST arrays of `count` DEVICE pointers to [M][N[i]], fp32 or (both)
+ *            bf16.  base[i] == y[i] adds in place (the rows of tokens without an
+ *            adapter are then left alone); base == NULL counts as zero.
+ *            Otherwise y[i] overlaps neither x, base nor another y
+ *            (W2A8_ERR_SHAPE).
+ *   N        HOST array of `count` entries
+ * 1 <= adapters <= 1024, rank_max a multiple of 8 up to 128, M, N and K as
+ * elsewhere.  One launch, no workspace: the tokens are sorted by adapter inside
+ * it.  Repeated calls give equal bits, and a token's result does not depend on
+ * the other tokens' values.  The adapters are read after the previous kernel of
+ * the stream has completed, so they may be exchanged between calls.
+ */
+int w2a8_lora_grouped(const void *x_bf16, const int32_t *adapter, int adapters, int rank_max,
+                      const int32_t *rank, const float *scale, int count, const void *const *A,
+                      const void *const *B, const void *const *base, void *const *y, int y_is_bf16,
+                      const int *N, int M, int K, void *stream);
+
+/*
+ * w2a8_rope_frequencies -- HOST only: the angle per position, in radians, of
+ * each of the rot_dim / 2 pairs, and the factor of their sines and cosines, for
+ * w2a8_rope and w2a8_qk_norm_rope.  f_p = base^(-2p / rot_dim), then
+ *   W2A8_ROPE_PLAIN   f_p
+ *   W2A8_ROPE_LINEAR  f_p / factor (positions are interpolated)
+ *   W2A8_ROPE_NTK     as PLAIN with base * factor^(rot_dim / (rot_dim - 2))
+ *   W2A8_ROPE_LLAMA3  by the full turns u = original_length f_p / 2 pi of a pair:
+ *                     f_p for u >= high, f_p / factor for u <= low, mixed
+ *                     linearly in u between
+ *   W2A8_ROPE_YARN    by the number of the pair: f_p up to the pair that makes
+ *                     `high` full turns within original_length (rounded down),
+ *                     f_p / factor from the one that makes `low` (rounded up),
+ *                     mixed linearly between; amplitude 0.1 ln(factor) + 1
+ * factor >= 1, base > 1; low, high (0 < low < high) and original_length count
+ * for LLAMA3 and YARN alone.
+ *   inv_freq   HOST, [rot_dim / 2] double;  amplitude  HOST, one float
+ */
+#define W2A8_ROPE_PLAIN 0
+#define W2A8_ROPE_LINEAR 1
+#define W2A8_ROPE_NTK 2
+#define W2A8_ROPE_LLAMA3 3
+#define W2A8_ROPE_YARN 4
+int w2a8_rope_frequencies(int rot_dim, double base, int scaling, double factor, double low, double high,
+                          int original_length, double *inv_freq, float *amplitude);
+
+/*
+ * w2a8_rope -- rotary positions on the rows of `count` (1 .. 4) results, e.g. the
+ * q and k of w2a8_linear_grouped.  (The paper has no counterpart.)  A head of
+ * head_dim values has rot_dim / 2 pairs (u, v): values p and p + rot_dim / 2, or
+ * 2 p and 2 p + 1 with `interleaved`.  With theta = positions[m] * inv_freq[p]:
+ *   u' = amplitude * (u cos theta - v sin theta)
+ *   v' = amplitude * (v cos theta + u sin theta)
+ * Values from rot_dim on pass through.  theta is formed in 64 bits (positions of
+ * any size), the rest is fp32, rounded once.  Positions may be negative: the
+ * rotation by -position undoes one, or moves rows that were rotated before.
+ *   x, out       HOST arrays of `count` DEVICE pointers; fp32 or bf16 each
+ *                (x_is_bf16, out_is_bf16), 16-byte aligned
+ *   heads        HOST, [count]: heads of result i
+ *   x_strides, out_strides   HOST, [count][2]: elements between tokens and
+ *                between heads; the values of a head are consecutive.  Rows of
+ *                `out` may not share elements; out[i] may be x[i] (same type and
+ *                strides), and otherwise no out overlaps an x or another out
+ *                (W2A8_ERR_SHAPE).  Column ranges of the same wider rows do not
+ *                overlap.  Elements between the rows are neither read nor written.
+ *   positions    [M] int32;  inv_freq  [rot_dim / 2] double (8-byte alignment)
+ * head_dim even, 2 .. 512; rot_dim even, 2 .. head_dim.  Head sizes, rot_dim and
+ * strides that are multiples of 8 take 16-byte accesses.
+ */
+int w2a8_rope(int count, const void *const *x, int x_is_bf16, void *const *out, int out_is_bf16, const int *heads,
+              const int64_t *x_strides, const int64_t *out_strides, int M, int head_dim, int rot_dim, int interleaved,
+              const int32_t *positions, const double *inv_freq, float amplitude, void *stream);
+
+/*
+ * w2a8_qk_norm_rope -- w2a8_rope with a norm of every head before the rotation,
+ * in the same pass: x * weight[i] / sqrt(mean(x^2) + eps), the mean over the
+ * head_dim values of one head, in fp32.
+ *   weight   HOST array of `count` DEVICE pointers to [head_dim] fp32, an entry
+ *            (or the array) NULL = 1;  eps >= 0
+ * The rest as for w2a8_rope; rot_dim may be 0 here (norms without a rotation;
+ * positions and inv_freq may then be NULL).
+ */
+int w2a8_qk_norm_rope(int count, const void *const *x, int x_is_bf16, void *const *out, int out_is_bf16,
+                      const float *const *weight, float eps, const int *heads, const int64_t *x_strides,
+                      const int64_t *out_strides, int M, int head_dim, int rot_dim, int interleaved,
+                      const int32_t *positions, const double *inv_freq, float amplitude, void *stream);
+
+/*
  * w2a8_read_probe -- measurement aid, not part of the method (the paper's
  * counterpart is the bandwidth roofline of Sec. II-E, which needs the machine's
  * attainable read bandwidth): one kernel that reads `bytes` bytes of `buffer`

@@ -22,6 +22,7 @@ EXPORTS = [
     "w2a8_gemm_grouped", "w2a8_linear_grouped", "w2a8_grouped_workspace_bytes", "w2a8_grouped_plan",
     "w2a8_read_probe", "w2a8_tensor_core_kind",
     "w2a8_linear_grouped_host", "w2a8_linear_grouped_host_workspace_bytes",
+    "w2a8_lora_grouped", "w2a8_rope_frequencies", "w2a8_rope", "w2a8_qk_norm_rope",
 ]
 
 _lib = None
@@ -80,6 +81,13 @@ def lib() -> ctypes.CDLL:
         L.w2a8_tensor_core_kind.restype = i
         L.w2a8_read_probe.argtypes = [vp, sz, vp, vp]
         L.w2a8_read_probe.restype = i
+        f, d = ctypes.c_float, ctypes.c_double
+        L.w2a8_lora_grouped.argtypes = [vp, vp, i, i, vp, vp, i, vp, vp, vp, vp, i, vp, i, i, vp]
+        L.w2a8_rope_frequencies.argtypes = [i, d, i, d, d, d, i, vp, vp]
+        L.w2a8_rope.argtypes = [i, vp, i, vp, i, vp, vp, vp, i, i, i, i, vp, vp, f, vp]
+        L.w2a8_qk_norm_rope.argtypes = [i, vp, i, vp, i, vp, f, vp, vp, vp, i, i, i, i, vp, vp, f, vp]
+        for name in ("w2a8_lora_grouped", "w2a8_rope_frequencies", "w2a8_rope", "w2a8_qk_norm_rope"):
+            getattr(L, name).restype = i
         for name in ("w2_pack", "a8_quantize", "w2a8_workspace_init", "w2a8_workspace_status", "w2a8_gemm",
                      "w2a8_gemm_partials", "w2a8_linear", "w2a8_linear_host", "w2a8_gemm_static",
                      "w2a8_gemm_grouped", "w2a8_linear_grouped", "w2a8_grouped_plan"):
@@ -373,6 +381,183 @@ def w2a8_linear_grouped_host(x_host: torch.Tensor, grp: Group, group: int, y_hos
                                           _ptr(workspace), workspace.numel() * workspace.element_size(),
                                           _stream(stream)), "w2a8_linear_grouped_host")
     return y_host
+
+
+def _want(t: torch.Tensor, name: str, dtype, shape, device):
+    """The tensor as the C entry points expect it: type, shape, device, rows without gaps."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}".replace("torch.", ""))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _on_current_device(device, stream):
+    """The launch goes to the current device: tensors of another one are refused, and so is a stream of another."""
+    if device.type != "cuda":
+        raise ValueError(f"tensors are on {device}: a CUDA device is needed")
+    here = torch.cuda.current_device()
+    if device.index != here or (stream is not None and stream.device.index != here):
+        raise ValueError(f"tensors or stream are on another device than the current one (cuda:{here})")
+
+
+class LoraGroup:
+    """Host-side argument block of w2a8_lora_grouped: the adapters of the matrices that share their activations,
+    A[i] bf16 [adapters][rank_max][K] and B[i] bf16 [adapters][N_i][rank_max], with `rank` (int32 [adapters], None:
+    rank_max) and `scale` (fp32 [adapters], None: 1).  Built once and reused every call; the tensors are held, so
+    their values may change between calls."""
+
+    def __init__(self, A, B, rank=None, scale=None):
+        self.A, self.B, self.rank, self.scale = list(A), list(B), rank, scale
+        self.count = len(self.A)
+        if self.count < 1 or len(self.B) != self.count:
+            raise ValueError("A and B must be lists of one tensor per matrix")
+        self.adapters, self.rank_max, self.K = (int(n) for n in self.A[0].shape)
+        self.N = [int(b.shape[1]) for b in self.B]
+        self.device = self.A[0].device
+        for a, b, n in zip(self.A, self.B, self.N):
+            _want(a, "A", torch.bfloat16, (self.adapters, self.rank_max, self.K), self.device)
+            _want(b, "B", torch.bfloat16, (self.adapters, n, self.rank_max), self.device)
+        if rank is not None:
+            _want(rank, "rank", torch.int32, (self.adapters,), self.device)
+        if scale is not None:
+            _want(scale, "scale", torch.float32, (self.adapters,), self.device)
+        ptrs = ctypes.c_void_p * self.count
+        self._a, self._b = ptrs(*[_ptr(t) for t in self.A]), ptrs(*[_ptr(t) for t in self.B])
+        self._n = (ctypes.c_int * self.count)(*self.N)
+        self._ptrs = ptrs
+
+    def _outputs(self, name, tensors, M, dtype):
+        if len(tensors) != self.count:
+            raise ValueError(f"{name} must have one tensor per matrix")
+        for t, n in zip(tensors, self.N):
+            _want(t, name, dtype, (M, n), self.device)
+        return self._ptrs(*[t.data_ptr() for t in tensors])
+
+
+def w2a8_lora_grouped(x: torch.Tensor, adapter: torch.Tensor, lora: LoraGroup, base=None, y=None,
+                      out_dtype: torch.dtype = torch.float32, stream=None):
+    """y[i] = base[i] + the adapters of x's tokens on matrix i (adapter int32 [M]; outside [0, adapters): none), e.g.
+    on the results of w2a8_linear_grouped.  base: list of [M][N_i] (fp32, or all bf16) or None = 0; y: list of outputs,
+    may be `base` itself (in place), None: new ones.  See w2a8_lora_grouped in include/w2a8.h."""
+    M = int(x.shape[0])
+    _on_current_device(lora.device, stream)
+    _want(x, "x", torch.bfloat16, (M, lora.K), lora.device)
+    _want(adapter, "adapter", torch.int32, (M,), lora.device)
+    dtype = (base if base is not None else y)[0].dtype if base is not None or y is not None else out_dtype
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("base and y must be float32 or bfloat16")
+    if y is None:
+        y = [torch.empty((M, n), dtype=dtype, device=lora.device) for n in lora.N]
+    py = lora._outputs("y", y, M, dtype)
+    pb = None if base is None else py if base is y else lora._outputs("base", base, M, dtype)
+    _check(lib().w2a8_lora_grouped(x.data_ptr(), adapter.data_ptr(), lora.adapters, lora.rank_max, _ptr(lora.rank),
+                                   _ptr(lora.scale), lora.count, lora._a, lora._b, pb, py,
+                                   1 if dtype == torch.bfloat16 else 0, lora._n, M, lora.K, _stream(stream)),
+           "w2a8_lora_grouped")
+    return y
+
+
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "ntk": 2, "llama3": 3, "yarn": 4}
+
+
+def w2a8_rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
+                          low: float = 1.0, high: float = 32.0, original_length: int = 0, device="cuda"):
+    """(inv_freq float64 [rot_dim / 2] on `device`, amplitude) for the rope entry points; scaling: a key of
+    ROPE_SCALINGS.  low / high: the full turns within original_length between which "llama3" and "yarn" mix.  See
+    w2a8_rope_frequencies in include/w2a8.h."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {sorted(ROPE_SCALINGS)}")
+    freq = torch.empty(max(int(rot_dim) // 2, 1), dtype=torch.float64)
+    amplitude = ctypes.c_float()
+    _check(lib().w2a8_rope_frequencies(rot_dim, base, ROPE_SCALINGS[scaling], factor, low, high, original_length,
+                                       _ptr(freq), ctypes.addressof(amplitude)), "w2a8_rope_frequencies")
+    return freq.to(device), float(amplitude.value)
+
+
+class Heads:
+    """Host-side argument block of the rope entry points: results x[i] [M][heads_i][head_dim] (fp32, or all bf16;
+    views with strides are fine as long as the values of a head are consecutive), the outputs, and the norms' weights
+    (fp32 [head_dim] or None, one per result).  out: a list of the same shapes (fp32 or bf16), `x` itself for in
+    place, or None: new ones of out_dtype (None: x's).  Built once and reused every call."""
+
+    def __init__(self, x, out=None, weight=None, out_dtype=None):
+        self.x = list(x)
+        self.count = len(self.x)
+        if not 1 <= self.count <= 4:
+            raise ValueError("1 to 4 results")
+        self.M, _, self.head_dim = (int(n) for n in self.x[0].shape)
+        self.device, self.dtype = self.x[0].device, self.x[0].dtype
+        if out is None:
+            out = [torch.empty(t.shape, dtype=out_dtype or self.dtype, device=self.device) for t in self.x]
+        self.out = list(out)
+        self.weight = [None] * self.count if weight is None else list(weight)
+        if len(self.out) != self.count or len(self.weight) != self.count:
+            raise ValueError("x, out and weight must have one entry per result")
+        self.out_dtype = self.out[0].dtype
+        for what, tensors, dtype in (("x", self.x, self.dtype), ("out", self.out, self.out_dtype)):
+            if dtype not in (torch.float32, torch.bfloat16):
+                raise TypeError(f"{what} must be float32 or bfloat16")
+            for t, like in zip(tensors, self.x):
+                if t.dtype != dtype:
+                    raise TypeError(f"{what}: tensors of one type")
+                if t.dim() != 3 or t.shape != like.shape or t.shape[0] != self.M or t.shape[2] != self.head_dim:
+                    raise ValueError(f"{what} must be [tokens][heads][head_dim]")
+                if t.device != self.device:
+                    raise ValueError(f"{what} is on {t.device}, not on {self.device}")
+                if t.stride(2) != 1:
+                    raise ValueError(f"{what}: the values of a head must be consecutive")
+        for w in self.weight:
+            if w is not None:
+                _want(w, "weight", torch.float32, (self.head_dim,), self.device)
+        ptrs, strides = ctypes.c_void_p * self.count, ctypes.c_int64 * (2 * self.count)
+        self._x, self._out = ptrs(*[_ptr(t) for t in self.x]), ptrs(*[_ptr(t) for t in self.out])
+        self._w = ptrs(*[_ptr(w) for w in self.weight])
+        self._xs = strides(*[t.stride(d) for t in self.x for d in (0, 1)])
+        self._os = strides(*[t.stride(d) for t in self.out for d in (0, 1)])
+        self._heads = (ctypes.c_int * self.count)(*[int(t.shape[1]) for t in self.x])
+
+
+def _rope_positions(heads: Heads, positions, inv_freq, stream):
+    _on_current_device(heads.device, stream)
+    if inv_freq is None:
+        return 0
+    rot = 2 * int(inv_freq.shape[0])
+    _want(inv_freq, "inv_freq", torch.float64, (rot // 2,), heads.device)
+    _want(positions, "positions", torch.int32, (heads.M,), heads.device)
+    return rot
+
+
+def w2a8_rope(heads: Heads, positions: torch.Tensor, inv_freq: torch.Tensor, amplitude: float = 1.0,
+              interleaved: bool = False, stream=None):
+    """Rotary positions (int32 [M]) on the results of `heads`; the first 2 * len(inv_freq) values of a head turn.
+    inv_freq (float64) and amplitude: from w2a8_rope_frequencies.  Returns heads.out.  See w2a8_rope in
+    include/w2a8.h."""
+    if inv_freq is None:
+        raise TypeError("inv_freq must be a float64 tensor")
+    rot = _rope_positions(heads, positions, inv_freq, stream)
+    _check(lib().w2a8_rope(heads.count, heads._x, heads.dtype == torch.bfloat16, heads._out,
+                           heads.out_dtype == torch.bfloat16, heads._heads, heads._xs, heads._os, heads.M,
+                           heads.head_dim, rot, 1 if interleaved else 0, positions.data_ptr(), inv_freq.data_ptr(),
+                           amplitude, _stream(stream)), "w2a8_rope")
+    return heads.out
+
+
+def w2a8_qk_norm_rope(heads: Heads, eps: float, positions: torch.Tensor | None = None,
+                      inv_freq: torch.Tensor | None = None, amplitude: float = 1.0, interleaved: bool = False,
+                      stream=None):
+    """The norm of every head (times heads.weight) and the rotation in one pass; without inv_freq the norm alone.
+    Returns heads.out.  See w2a8_qk_norm_rope in include/w2a8.h."""
+    rot = _rope_positions(heads, positions, inv_freq, stream)
+    _check(lib().w2a8_qk_norm_rope(heads.count, heads._x, heads.dtype == torch.bfloat16, heads._out,
+                                   heads.out_dtype == torch.bfloat16, heads._w, eps, heads._heads, heads._xs,
+                                   heads._os, heads.M, heads.head_dim, rot, 1 if interleaved else 0,
+                                   _ptr(positions) if rot else 0, _ptr(inv_freq), amplitude, _stream(stream)),
+           "w2a8_qk_norm_rope")
+    return heads.out
 
 
 def w2a8_read_probe(buffer: torch.Tensor, sink: torch.Tensor, stream=None):
