@@ -10,15 +10,16 @@
 // One launch, no workspace.  Every CTA sorts the tokens of the batch by adapter itself (a stable counting sort of
 // 4096 tokens at a time in shared memory: all CTAs find the same order) and cuts them into tiles of up to 64 tokens
 // of one adapter.  A work item is (tile, matrix, share of the channels); a cluster of C CTAs takes one at a time:
-//   1. h: the K axis is split over the CTAs of the cluster and the warps of a CTA; mma.sync bf16 with the operands
-//      straight from global memory (k is permuted alike on both sides so that a lane's operands of two instructions
-//      are 16 consecutive bytes).  Sums of the warps are added in shared memory, of the CTAs over the cluster, both
-//      in a fixed order.
+//   1. h: the K axis is split over the CTAs of the cluster, and inside a CTA over pairs of warps; tokens and ranks over
+//      the other warps.  The sums are added in a fixed order, over the cluster through distributed shared memory.
 //   2. y: the channels of the item are split over the CTAs and warps.  s h stays in fp32: it is cut into three bf16
 //      terms by truncation, whose sum is exactly its 24 bits (two terms, 16 bits, for a bf16 result), so the product
-//      with the bf16 B carries no rounding of h.  Channels are permuted so that a lane holds four consecutive ones.
-#include <type_traits>
-
+//      with the bf16 B carries no rounding of h.
+// Both steps are fed by one ring of shared-memory stages that cp.async fills ahead (x and A, then B and base), so
+// that the loads of step 2 are on their way while the sums of step 1 are added.  mma.sync bf16: the ranks a tile has
+// fill 16 to 128 columns, far too few for tcgen05 tiles to pay, and the bytes bound the kernel.  k is permuted alike on
+// both sides so that a lane's operands of two instructions are 16 consecutive bytes, and the channels so that a lane
+// holds four consecutive ones.
 #include "w2a8_common.cuh"
 
 namespace w2a8 {
@@ -28,8 +29,6 @@ constexpr int kLoraMaxAdapters = 1024;
 constexpr int kLoraMaxRank = 128;
 constexpr int kLoraThreads = 256;
 constexpr int kLoraWarps = kLoraThreads / 32;
-constexpr int kLoraTile = 64;            // tokens per tile
-constexpr int kLoraChunk = 4096;         // tokens that are sorted at a time
 constexpr int kLoraMaxCluster = 8;
 
 struct LoraParams {
@@ -51,26 +50,55 @@ __device__ __forceinline__ float4 lora_ld_cluster(uint32_t local, uint32_t rank)
                  : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote) : "memory");
     return v;
 }
+__device__ __forceinline__ void lora_copy16(uint32_t to, const void *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+// the first `bytes` of 16, zeros behind them
+__device__ __forceinline__ void lora_copy_some(uint32_t to, const void *from, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ uint4 lora_lds128(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint2 lora_lds64(uint32_t at) {
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+    return v;
+}
 
-// Shared memory of an instance: RK ranks at most, RP of them in a pass of step 1.
-template <int RK>
+// An instance: tiles of T tokens, ranks of up to RK.  Everything that an address in the loops below depends on is a
+// constant of it.  Two CTAs per SM up to 64 ranks; with 128 the terms of s h need the registers of a whole SM.
+template <int T_, int RK_>
+struct LoraCfg {
+    static constexpr int T = T_, RK = RK_;
+    static constexpr int kChunk = T == 16 ? kLoraThreads : 4096;      // tokens that are sorted at a time
+    static constexpr int MT = T / 16, NT = RK / 8;
+    static constexpr int NR = MT == 4 ? 2 : NT < 8 ? NT : 8;          // step 1: shares of the ranks among the warps
+    static constexpr int NK = kLoraWarps / MT / NR;                   // and of K
+    static constexpr int WN = kLoraWarps / MT;                        // step 2: shares of the channels
+    static constexpr int KC = T == 64 ? 64 : RK == 16 ? 256 : RK <= 64 ? 128 : 64;      // values of K per stage
+    static constexpr int CH = T == 64 ? (RK <= 64 ? 32 : 64) : 128;   // channels per stage
+    static constexpr int kBytes1 = (T + RK) * KC * 2, kBytes2 = CH * (2 * RK + 4 * T);
+    static constexpr int kStageBytes = kBytes1 > kBytes2 ? kBytes1 : kBytes2;
+    static constexpr int kStages = 4;
+    static constexpr int kBlocksPerSm = RK <= 64 ? 2 : 1;
+    static constexpr int HSTR = RK + 4;          // floats between rows of h: no bank conflicts
+};
+template <typename Cfg>
 struct LoraSmem {
-    static constexpr int RP = RK < 64 ? RK : 64;
-    static constexpr int RSTR = RP + 4;          // floats between rows of a warp's sums: no bank conflicts
-    static constexpr int HSTR = RK + 4;          // of h
-    union Scratch {
-        struct {
-            uint16_t hist[kLoraWarps][kLoraMaxAdapters + 1];
-            uint16_t within[kLoraChunk];         // place of a token among those of its warp and adapter
-        } sort;
-        float sums[kLoraWarps][16 * RSTR];       // per warp
-        float h[kLoraTile * HSTR];               // after the cluster's sum: s h
+    union Ring {
+        char stage[Cfg::kStages][Cfg::kStageBytes];
+        uint16_t hist[kLoraWarps * (kLoraMaxAdapters + 1)];           // of the sort: tokens of each adapter by warp
     };
-    alignas(16) Scratch u;
-    alignas(16) float part[kLoraTile * HSTR];    // this CTA's share of K, read by the cluster
-    uint16_t perm[kLoraChunk];                   // tokens of the chunk in order of their adapters
+    alignas(128) Ring ring;
+    alignas(16) float part[Cfg::T * Cfg::HSTR];  // this CTA's share of K, read by the cluster
+    alignas(16) float h[Cfg::T * Cfg::HSTR];     // s h, all of K
+    uint16_t perm[Cfg::kChunk];                  // tokens of the chunk in order of their adapters
     uint16_t first[kLoraMaxAdapters + 2];        // first place in perm of each adapter's tokens
     uint16_t tiles[kLoraMaxAdapters + 2];        // tiles of the adapters before this one
+    uint8_t rank[kLoraMaxAdapters + 1];          // ranks, clamped; 0 for none
     uint32_t scan[kLoraWarps];
 };
 
@@ -79,8 +107,8 @@ __device__ __forceinline__ uint32_t pack_hi16(float lo, float hi) {      // the 
 }
 __device__ __forceinline__ float trunc_bf16(float v) { return __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); }
 
-// Cut v into T bf16 terms by truncation: 8 significant bits each, the differences are exact.  An infinity or NaN is
-// its own first term.
+// Cut a and b into T bf16 terms by truncation: 8 significant bits each, the differences are exact.  An infinity or NaN
+// is its own first term.
 template <int T>
 __device__ __forceinline__ void cut_pair(float a, float b, uint32_t (&term)[T]) {
 #pragma unroll
@@ -93,333 +121,422 @@ __device__ __forceinline__ void cut_pair(float a, float b, uint32_t (&term)[T]) 
     }
 }
 
-// keep the first `n` of eight / four bf16 values (n <= 0: none)
-__device__ __forceinline__ uint32_t keep2(uint32_t w, int n) { return n >= 2 ? w : n == 1 ? (w & 0xFFFFu) : 0u; }
+// The tokens of a chunk in order of their adapters (perm), where each adapter's begin (first) and the tiles before it
+// (tiles); adapter `L` stands for none.
+template <typename Cfg>
+__device__ __forceinline__ void lora_sort(LoraSmem<Cfg> &sm, const LoraParams &p, int chunk, int n_tok) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, L = p.adapters;
+    uint16_t *hist = sm.ring.hist, *mine = hist + warp * (L + 1);
+    for (int i = tid; i < kLoraWarps * (L + 1); i += kLoraThreads) hist[i] = 0;
+    __syncthreads();
+    constexpr int kSteps = Cfg::kChunk / kLoraThreads, T = Cfg::T;
+    const int steps = (n_tok + kLoraThreads - 1) / kLoraThreads;
+    const int w0 = warp * steps * 32 + lane;
+    int own[kSteps], place[kSteps];              // adapter of the lane's tokens (-1: no token), place among those of the warp
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+        own[i] = -1;
+        if (i < steps && w0 + i * 32 < n_tok) {
+            const int a = p.adapter[chunk + w0 + i * 32];
+            own[i] = a < 0 || a >= L ? L : a;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+        if (i >= steps) continue;
+        const unsigned same = __match_any_sync(0xFFFFFFFFu, own[i]);
+        const int before = __popc(same & ((1u << lane) - 1u));
+        const int had = own[i] >= 0 ? mine[own[i]] : 0;
+        place[i] = had + before;
+        __syncwarp();
+        if (own[i] >= 0 && before == 0) mine[own[i]] = (uint16_t)(had + __popc(same));
+        __syncwarp();
+    }
+    __syncthreads();
+    // exclusive sums over the adapters, of tokens (low half) and of tiles (high half); a thread has `each` of them
+    const int each = (L + 1 + kLoraThreads - 1) / kLoraThreads;
+    const int a0 = min(L + 1, tid * each), a1 = min(L + 1, a0 + each);
+    uint32_t total = 0;
+    for (int a = a0; a < a1; ++a) {
+        uint32_t n = 0;
+        for (int w = 0; w < kLoraWarps; ++w) {
+            const uint32_t c = hist[w * (L + 1) + a];
+            hist[w * (L + 1) + a] = (uint16_t)n;                     // tokens of this adapter in the warps before
+            n += c;
+        }
+        sm.first[a] = (uint16_t)n;
+        total += n + ((n + T - 1) / T << 16);
+    }
+    uint32_t incl = total;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += v;
+    }
+    if (lane == 31) sm.scan[warp] = incl;
+    __syncthreads();
+    uint32_t at = incl - total;
+    for (int w = 0; w < warp; ++w) at += sm.scan[w];
+    for (int a = a0; a < a1; ++a) {
+        const uint32_t n = sm.first[a];
+        sm.first[a] = (uint16_t)at;
+        sm.tiles[a] = (uint16_t)(at >> 16);
+        at += n + ((n + T - 1) / T << 16);
+    }
+    if (a0 < a1 && a1 == L + 1) { sm.first[L + 1] = (uint16_t)at; sm.tiles[L + 1] = (uint16_t)(at >> 16); }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+        if (own[i] >= 0) sm.perm[sm.first[own[i]] + mine[own[i]] + place[i]] = (uint16_t)(w0 + i * 32);
+    __syncthreads();
+}
 
-template <int RK, bool Y16>
-__global__ void __launch_bounds__(kLoraThreads)
+template <int T, int RK, bool Y16>
+__global__ void __launch_bounds__(kLoraThreads, LoraCfg<T, RK>::kBlocksPerSm)
 w2a8_lora_kernel(const LoraParams p) {
-    using Smem = LoraSmem<RK>;
-    constexpr int RP = Smem::RP, NT = RP / 8, RSTR = Smem::RSTR, HSTR = Smem::HSTR;
+    using Cfg = LoraCfg<T, RK>;
+    using Smem = LoraSmem<Cfg>;
+    constexpr int MT = Cfg::MT, NR = Cfg::NR, NK = Cfg::NK, NTW = Cfg::NT / NR, WN = Cfg::WN, KC = Cfg::KC, CH = Cfg::CH;
+    constexpr int HSTR = Cfg::HSTR, S = Cfg::kStages, STAGE = Cfg::kStageBytes;
     constexpr int TERMS = Y16 ? 2 : 3;
     constexpr int KS = RK / 16;                  // steps of 16 ranks in step 2
-    extern __shared__ __align__(16) char smem_raw[];
+    constexpr int E = Y16 ? 2 : 4;               // bytes of a value of base and y
+    extern __shared__ __align__(128) char smem_raw[];
     Smem &sm = *reinterpret_cast<Smem *>(smem_raw);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int g = lane >> 2, t = lane & 3;       // row and column pair of a lane in the tiles of mma.sync
     const int C = p.C, crank = C > 1 ? (int)cluster_ctarank() : 0;
     const int cluster = blockIdx.x / C, clusters = gridDim.x / C;
     const int L = p.adapters;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(sm.ring.stage[0]);
+    // Warps: MT tiles of 16 tokens, in step 1 times NR shares of the ranks and NK of K, in step 2 times WN of the channels.
+    const int wm = warp % MT, wr = warp / MT, jr = wr % NR, jk = wr / NR;
+    const int ra = wm * 16 + g, rb = ra + 8;                          // the lane's two tokens in the tile
+    const int units = p.K / 64, u_per = units / C, u_more = units - u_per * C;
+    const int u0 = crank * u_per + min(crank, u_more), n_units = u_per + (crank < u_more);
+    constexpr int KU = KC / 64;
+    const int n1 = (n_units + KU - 1) / KU;
+
+    // Stages.  Step 1: T rows of x, RK of A, KC values each; step 2: CH rows of B, RK values each, and T rows of base, CH
+    // values each.  16-byte pieces, with an odd row's halves of 128 bytes exchanged where rows are multiples of 128
+    // bytes, so that the reads below meet no bank conflicts.  A thread copies the same column of rows that are an even
+    // number apart, so that its addresses only move on from stage to stage.
+    constexpr int CPX = KC / 8, DX = kLoraThreads / CPX, PX = (T + DX - 1) / DX, PA = (RK + DX - 1) / DX;
+    constexpr int CPB = RK / 8, DB = kLoraThreads / CPB, PB = (CH + DB - 1) / DB;
+    constexpr int CPY = CH * E / 16, DY = kLoraThreads / CPY, PY = (T + DY - 1) / DY;
+    constexpr uint32_t FB = RK >= 64 ? 4u : 0u, FY = E == 4 ? 4u : 0u;
+    constexpr uint32_t kA = T * KC * 2, kBase = CH * RK * 2;          // of A and base in a stage
+    const int cx = tid % CPX, rx = tid / CPX, cb = tid % CPB, rbb = tid / CPB, cy = tid % CPY, ry = tid / CPY;
+    const uint32_t to_x = rx * (KC * 2) + ((cx ^ ((rx & 1) << 2)) << 4);
+    const uint32_t to_b = rbb * (RK * 2) + ((cb ^ ((rbb & 1) * FB)) << 4);
+    const uint32_t to_y = kBase + ry * (CH * E) + ((cy ^ ((ry & 1) * FY)) << 4);
     pdl_launch_dependents();
     pdl_wait();
+    for (int a = tid; a <= L; a += kLoraThreads)
+        sm.rank[a] = (uint8_t)(a == L ? 0 : p.rank ? min(max(p.rank[a], 0), p.rank_max) : p.rank_max);
 
     bool reading = false;                        // an open cluster barrier phase: others may read `part`
     int turn = 0;                                // items of the chunks before, modulo the clusters
-    for (int chunk = 0; chunk < p.M; chunk += kLoraChunk) {
-        const int n_tok = min(kLoraChunk, p.M - chunk);
-        // ---- sort: places of the tokens, adapter `L` standing for none ------------------------------------------
+    for (int chunk = 0; chunk < p.M; chunk += Cfg::kChunk) {
         __syncthreads();
-        for (int i = tid; i < kLoraWarps * (kLoraMaxAdapters + 1); i += kLoraThreads) {
-            const int a = i % (kLoraMaxAdapters + 1);
-            if (a <= L) (&sm.u.sort.hist[0][0])[i] = 0;
-        }
-        __syncthreads();
-        const int per_warp = (n_tok + kLoraThreads - 1) / kLoraThreads * 32;
-        const int w0 = min(n_tok, warp * per_warp), w1 = min(n_tok, w0 + per_warp);
-        auto adapter_of = [&](int i) {
-            const int a = p.adapter[chunk + i];
-            return a < 0 || a >= L ? L : a;
-        };
-        for (int i0 = w0; i0 < w1; i0 += 32) {
-            const int i = i0 + lane;
-            const int a = i < w1 ? adapter_of(i) : -1;
-            const unsigned same = __match_any_sync(0xFFFFFFFFu, a);
-            const int before = __popc(same & ((1u << lane) - 1u));
-            int had = 0;
-            if (a >= 0) had = sm.u.sort.hist[warp][a];
-            __syncwarp();
-            if (a >= 0) {
-                sm.u.sort.within[i] = (uint16_t)(had + before);
-                if (before == 0) sm.u.sort.hist[warp][a] = (uint16_t)(had + __popc(same));
-            }
-            __syncwarp();
-        }
-        __syncthreads();
-        // exclusive sums over the adapters, of tokens (low half) and of tiles (high half); thread i has `each` of them
-        {
-            const int each = (L + 1 + kLoraThreads - 1) / kLoraThreads;
-            const int a0 = min(L + 1, tid * each), a1 = min(L + 1, a0 + each);
-            uint32_t mine = 0;
-            for (int a = a0; a < a1; ++a) {
-                uint32_t n = 0;
-                for (int w = 0; w < kLoraWarps; ++w) {
-                    const uint32_t c = sm.u.sort.hist[w][a];
-                    sm.u.sort.hist[w][a] = (uint16_t)n;              // tokens of this adapter in the warps before
-                    n += c;
-                }
-                sm.first[a] = (uint16_t)n;
-                mine += n + ((n + kLoraTile - 1) / kLoraTile << 16);
-            }
-            uint32_t incl = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-                if (lane >= o) incl += v;
-            }
-            if (lane == 31) sm.scan[warp] = incl;
-            __syncthreads();
-            uint32_t at = incl - mine;
-            for (int w = 0; w < warp; ++w) at += sm.scan[w];
-            for (int a = a0; a < a1; ++a) {
-                const uint32_t n = sm.first[a];
-                sm.first[a] = (uint16_t)at;
-                sm.tiles[a] = (uint16_t)(at >> 16);
-                at += n + ((n + kLoraTile - 1) / kLoraTile << 16);
-            }
-            if (a1 == L + 1 && a0 < a1) { sm.first[L + 1] = (uint16_t)at; sm.tiles[L + 1] = (uint16_t)(at >> 16); }
-        }
-        __syncthreads();
-        for (int i0 = w0; i0 < w1; i0 += 32) {
-            const int i = i0 + lane;
-            if (i < w1) {
-                const int a = adapter_of(i);
-                sm.perm[sm.first[a] + sm.u.sort.hist[warp][a] + sm.u.sort.within[i]] = (uint16_t)i;
-            }
-        }
-        __syncthreads();
+        lora_sort<Cfg>(sm, p, chunk, min(Cfg::kChunk, p.M - chunk));
 
         // ---- the items of the chunk, dealt to the clusters in turn -------------------------------------------------
         const int n_tiles = sm.tiles[L + 1];
         const int whole = n_tiles * p.count;
-        const int shares = max(1, clusters / max(whole, 1));         // few items: several clusters share the channels of one
+        // Few items: several clusters share the channels of one.  Each of them does step 1 for itself, so not many more
+        // than the bytes of step 2 are to those of step 1.
+        int shares = 1;
+        if (2 * whole <= clusters) {
+            int widest = 0;
+            for (int i = 0; i < p.count; ++i) widest = max(widest, p.N[i]);
+            const float toks = (float)min(Cfg::kChunk, p.M - chunk) / n_tiles;
+            const float s1 = (toks + p.rank_max) * p.K, s2 = widest * (p.rank_max + E * toks);
+            shares = min(clusters / whole, 1 + (int)min(2.0f * s2 / s1, 64.0f));
+        }
         const int items = whole * shares;
         int item = cluster - turn;
         if (item < 0) item += clusters;
         for (; item < items; item += clusters) {
-            const int share = item % shares, tile = item / shares / p.count, mat = item / shares % p.count;
+            const int wi = item / shares, share = item - wi * shares, tile = wi / p.count, mat = wi - tile * p.count;
             int a = 0;                                                // adapter of the tile: the last with tiles[a] <= tile
-            for (int step = 1 << 10; step > 0; step >>= 1)
+            for (int step = 1 << (31 - __clz(L)); step > 0; step >>= 1)
                 if (a + step <= L && sm.tiles[a + step] <= tile) a += step;
-            const int at = sm.first[a] + (tile - sm.tiles[a]) * kLoraTile;
-            const int n = min(kLoraTile, sm.first[a + 1] - at);       // tokens of the tile
-            int r = 0;
-            float s = 1.0f;
-            if (a < L) {
-                r = p.rank ? min(max(p.rank[a], 0), p.rank_max) : p.rank_max;
-                if (p.scale) s = p.scale[a];
-            }
+            const int at = sm.first[a] + (tile - sm.tiles[a]) * T;
+            const int n = min(T, sm.first[a + 1] - at);               // tokens of the tile
+            const int r = sm.rank[a];
             const int N = p.N[mat];
-            const uint16_t *base16 = static_cast<const uint16_t *>(p.base[mat]);
-            const float *base32 = static_cast<const float *>(p.base[mat]);
-            uint16_t *y16 = static_cast<uint16_t *>(p.y[mat]);
-            float *y32 = static_cast<float *>(p.y[mat]);
+            const char *base = static_cast<const char *>(p.base[mat]);
+            char *y = static_cast<char *>(p.y[mat]);
             // blocks of 16 channels of this CTA
             const int blocks = N / 16, parts = shares * C, part_id = share * C + crank;
-            const int cb0 = (int)((long long)blocks * part_id / parts), cb1 = (int)((long long)blocks * (part_id + 1) / parts);
+            const int per = blocks / parts, more = blocks - per * parts;
+            const int ch0 = (part_id * per + min(part_id, more)) * 16, n_ch = (per + (part_id < more)) * 16;
 
             if (r == 0) {                                             // nothing to add
-                if (p.base[mat] == p.y[mat]) continue;
-                constexpr int VB = Y16 ? 2 : 4;                       // 16-byte vectors per block
-                const int per = (cb1 - cb0) * VB;
-                for (int i = tid; i < n * per; i += kLoraThreads) {
-                    const size_t off = (size_t)(chunk + sm.perm[at + i / per]) * N * (Y16 ? 2 : 4) +
-                                       (size_t)(cb0 * VB + i % per) * 16;
-                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                    if (base32) v = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(base32) + off);
-                    *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(y32) + off) = v;
+                if (base == y) continue;
+                const int row_v = n_ch * E / 16;
+                for (int i = tid; i < n * row_v; i += kLoraThreads) {
+                    const size_t off = ((size_t)(chunk + sm.perm[at + i / row_v]) * N + ch0) * E + (size_t)(i % row_v) * 16;
+                    *reinterpret_cast<uint4 *>(y + off) = base ? *reinterpret_cast<const uint4 *>(base + off) : make_uint4(0u, 0u, 0u, 0u);
                 }
                 continue;
             }
-
-            // warps: `mt` tiles of 16 tokens (1, 2 or 4) times shares of K (step 1) or of the channels (step 2)
-            const int mt = n <= 16 ? 1 : n <= 32 ? 2 : 4;
-            const int wm = warp & (mt - 1), wk = warp / mt, wn = kLoraWarps / mt;
-            const int ra = wm * 16 + g, rb = ra + 8;                  // the lane's two tokens in the tile
+            const float s = p.scale ? p.scale[a] : 1.0f;
             const bool live = wm * 16 < n, la = ra < n, lb = rb < n;
-            const int ta = chunk + (la ? sm.perm[at + ra] : 0), tb = chunk + (lb ? sm.perm[at + rb] : 0);
+            const int n2 = (n_ch + CH - 1) / CH;
+
+            const char *src_x[PX], *src_y[PY];
+#pragma unroll
+            for (int i = 0; i < PX; ++i) {
+                const int row = min(rx + i * DX, n - 1);              // rows behind the tile's tokens: no bytes of the last
+                src_x[i] = reinterpret_cast<const char *>(p.x + (size_t)(chunk + sm.perm[at + row]) * p.K + u0 * 64 + cx * 8);
+            }
+#pragma unroll
+            for (int i = 0; i < PY; ++i) {
+                const int row = min(ry + i * DY, n - 1);
+                src_y[i] = base + ((size_t)(chunk + sm.perm[at + row]) * N + ch0) * E + cy * 16;
+            }
+            const char *src_a = reinterpret_cast<const char *>(p.A[mat] + ((size_t)a * p.rank_max + rx) * p.K + u0 * 64 + cx * 8);
+            // the bytes of a piece of B that are ranks of the adapter: the rest counts as zero, whatever the row holds
+            const int b_bytes = min(max(r - cb * 8, 0), 8) * 2;
+            const char *src_b = reinterpret_cast<const char *>(p.B[mat] + ((size_t)a * N + ch0 + rbb) * p.rank_max + (b_bytes ? cb * 8 : 0));
+            int q_issue = 0, slot_issue = 0;
+            auto issue = [&]() {
+                const uint32_t st = ring + slot_issue * STAGE;
+                if (q_issue < n1) {
+                    if (KU == 1 || cx < (n_units - q_issue * KU) * 8) {
+#pragma unroll
+                        for (int i = 0; i < PX; ++i)
+                            if (T % DX == 0 || rx + i * DX < T)
+                                lora_copy_some(st + to_x + i * (kLoraThreads * 16), src_x[i], rx + i * DX < n ? 16 : 0);
+#pragma unroll
+                        for (int i = 0; i < PA; ++i)
+                            if (rx + i * DX < r)
+                                lora_copy16(st + kA + to_x + i * (kLoraThreads * 16), src_a + (size_t)(i * DX) * p.K * 2);
+                    }
+#pragma unroll
+                    for (int i = 0; i < PX; ++i) src_x[i] += KC * 2;
+                    src_a += KC * 2;
+                } else if (q_issue < n1 + n2) {
+                    const int cw = n_ch - (q_issue - n1) * CH;        // channels that are left
+#pragma unroll
+                    for (int i = 0; i < PB; ++i)
+                        if (rbb + i * DB < min(cw, CH))
+                            lora_copy_some(st + to_b + i * (kLoraThreads * 16), src_b + (size_t)(i * DB) * p.rank_max * 2, b_bytes);
+                    src_b += (size_t)CH * p.rank_max * 2;
+                    if (base && cy * (16 / E) < cw) {
+#pragma unroll
+                        for (int i = 0; i < PY; ++i)
+                            if (ry + i * DY < n) lora_copy16(st + to_y + i * (kLoraThreads * 16), src_y[i]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < PY; ++i) src_y[i] += CH * E;
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                ++q_issue;
+                slot_issue = slot_issue + 1 == S ? 0 : slot_issue + 1;
+            };
+            // every stage is one group, also an empty one: S - 2 groups may still be open when a stage is needed
+            int slot = 0;
+            auto arrive = [&]() {
+                asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
+                __syncthreads();
+                issue();
+                const uint32_t st = ring + slot * STAGE;
+                slot = slot + 1 == S ? 0 : slot + 1;
+                return st;
+            };
+            __syncthreads();                                          // the stages and h of the item before are done with
+#pragma unroll 1
+            for (int q = 0; q < S - 1; ++q) issue();
 
             // ---- step 1 -------------------------------------------------------------------------------------------
-            const int units = p.K / 64, slices = C * wn, slice = crank * wn + wk;
-            const uint16_t *xa = p.x + (size_t)ta * p.K + 8 * t, *xb = p.x + (size_t)tb * p.K + 8 * t;
-            const uint16_t *wrow = p.A[mat] + ((size_t)a * p.rank_max + g) * p.K + 8 * t;
-            const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-            for (int r0 = 0; r0 < r; r0 += RP) {
-                float acc[NT][4];
+            float acc[NTW][4];
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
-                if (live) {
-                    for (int u = slice; u < units; u += slices) {
-                        uint4 va[2], vb[2], w[NT][2];
+            for (int j = 0; j < NTW; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
+            const uint32_t flip = (g & 1) << 2;
+#pragma unroll 1
+            for (int q = 0; q < n1; ++q) {
+                const uint32_t st = arrive();
+                if (!live) continue;
+                const uint32_t xrow = st + ra * (KC * 2), arow = st + kA + (jr * NTW * 8 + g) * (KC * 2);
+                const int k32 = KU == 1 ? 2 : 2 * (n_units - q * KU);
 #pragma unroll
-                        for (int b = 0; b < 2; ++b) {
-                            va[b] = la ? *reinterpret_cast<const uint4 *>(xa + u * 64 + b * 32) : zero;
-                            vb[b] = lb ? *reinterpret_cast<const uint4 *>(xb + u * 64 + b * 32) : zero;
-                        }
+                for (int b0 = 0; b0 < 2 * KU; b0 += NK) {
+                    const int b = b0 + jk;
+                    if (KU > 1 && b >= k32) continue;
+                    const uint32_t col = ((4 * b + t) ^ flip) << 4;
+                    const uint4 va = lora_lds128(xrow + col), vb = lora_lds128(xrow + 8 * KC * 2 + col);
+                    uint4 w[NTW];
 #pragma unroll
-                        for (int j = 0; j < NT; ++j)
+                    for (int j = 0; j < NTW; ++j) w[j] = lora_lds128(arow + j * (8 * KC * 2) + col);
+                    // A sum of 32 products at a time joins the running one with a rounded addition: the instruction
+                    // truncates where it aligns its addends, a bias that a long chain would add up.
+                    float d[NTW][4] = {};
 #pragma unroll
-                            for (int b = 0; b < 2; ++b)
-                                w[j][b] = r0 + j * 8 + g < r
-                                              ? *reinterpret_cast<const uint4 *>(wrow + (size_t)(r0 + j * 8) * p.K + u * 64 + b * 32)
-                                              : zero;
+                    for (int j = 0; j < NTW; ++j) mma_bf16_16x8x16(d[j], va.x, vb.x, va.y, vb.y, w[j].x, w[j].y, d[j]);
 #pragma unroll
-                        for (int j = 0; j < NT; ++j) {
-                            if (r0 + j * 8 >= r) continue;
+                    for (int j = 0; j < NTW; ++j) mma_bf16_16x8x16(d[j], va.z, vb.z, va.w, vb.w, w[j].z, w[j].w, d[j]);
 #pragma unroll
-                            for (int b = 0; b < 2; ++b) {
-                                mma_bf16_16x8x16(acc[j], va[b].x, vb[b].x, va[b].y, vb[b].y, w[j][b].x, w[j][b].y, acc[j]);
-                                mma_bf16_16x8x16(acc[j], va[b].z, vb[b].z, va[b].w, vb[b].w, w[j][b].z, w[j][b].w, acc[j]);
-                            }
-                        }
+                    for (int j = 0; j < NTW; ++j)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) acc[j][c] += d[j][c];
+                }
+            }
+            if (reading) { cluster_wait(); reading = false; }         // the shares of the item before have been read
+#pragma unroll
+            for (int k = NK - 1; k >= 0; --k) {
+                if (jk == k && live) {
+#pragma unroll
+                    for (int j = 0; j < NTW; ++j) {
+                        const int col = (jr * NTW + j) * 8 + 2 * t;
+                        float2 *d0 = reinterpret_cast<float2 *>(&sm.part[ra * HSTR + col]);
+                        float2 *d1 = reinterpret_cast<float2 *>(&sm.part[rb * HSTR + col]);
+                        float2 v0 = make_float2(acc[j][0], acc[j][1]), v1 = make_float2(acc[j][2], acc[j][3]);
+                        if (k != NK - 1) { v0.x += d0->x; v0.y += d0->y; v1.x += d1->x; v1.y += d1->y; }
+                        *d0 = v0;
+                        *d1 = v1;
                     }
                 }
-                __syncthreads();                                      // `u` is free (sort, h or the sums before)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    float *d = &sm.u.sums[warp][g * RSTR + j * 8 + 2 * t];
-                    *reinterpret_cast<float2 *>(d) = make_float2(acc[j][0], acc[j][1]);
-                    *reinterpret_cast<float2 *>(d + 8 * RSTR) = make_float2(acc[j][2], acc[j][3]);
-                }
-                if (reading) { cluster_wait(); reading = false; }     // the shares of the item before have been read
-                __syncthreads();
-                for (int i = tid; i < mt * 16 * (RP / 4); i += kLoraThreads) {
-                    const int row = i / (RP / 4), c4 = i % (RP / 4);
-                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                    for (int k = 0; k < wn; ++k) {
-                        const float4 q = *reinterpret_cast<const float4 *>(
-                            &sm.u.sums[k * mt + (row >> 4)][(row & 15) * RSTR + c4 * 4]);
-                        v.x += q.x; v.y += q.y; v.z += q.z; v.w += q.w;
-                    }
-                    *reinterpret_cast<float4 *>(&sm.part[row * HSTR + r0 + c4 * 4]) = v;
-                }
+                if (k > 0) __syncthreads();
             }
             if (C > 1) cluster_sync(); else __syncthreads();
             {
-                // columns up to the next multiple of 16 ranks; those from r on count as zero, whatever the row holds
-                const int cols4 = (r + 15) / 16 * 4;
+                // columns of ranks that the adapter has not (sums with whatever the stage held) count as zero
+                constexpr int C4 = RK / 4;
                 const uint32_t part_u32 = (uint32_t)__cvta_generic_to_shared(sm.part);
-                for (int i = tid; i < mt * 16 * cols4; i += kLoraThreads) {
-                    const int off = (i / cols4) * HSTR + (i % cols4) * 4;
+                for (int i = tid; i < n * C4; i += kLoraThreads) {
+                    const int j = (i % C4) * 4, off = (i / C4) * HSTR + j;
                     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (C > 1) {
-                        for (int c = 0; c < C; ++c) {
-                            const float4 q = lora_ld_cluster(part_u32 + off * 4, c);
-                            v.x += q.x; v.y += q.y; v.z += q.z; v.w += q.w;
+                    if (j < r) {
+                        if (C > 1) {
+                            float4 o[kLoraMaxCluster];
+#pragma unroll
+                            for (int c = 0; c < kLoraMaxCluster; ++c)
+                                if (c < C) o[c] = lora_ld_cluster(part_u32 + off * 4, c);
+#pragma unroll
+                            for (int c = 0; c < kLoraMaxCluster; ++c)
+                                if (c < C) { v.x += o[c].x; v.y += o[c].y; v.z += o[c].z; v.w += o[c].w; }
+                        } else {
+                            v = *reinterpret_cast<const float4 *>(&sm.part[off]);
                         }
-                    } else {
-                        v = *reinterpret_cast<const float4 *>(&sm.part[off]);
+                        v.x *= s;
+                        v.y = j + 1 < r ? v.y * s : 0.0f;
+                        v.z = j + 2 < r ? v.z * s : 0.0f;
+                        v.w = j + 3 < r ? v.w * s : 0.0f;
                     }
-                    const int j = (i % cols4) * 4;
-                    v.x = j < r ? v.x * s : 0.0f;
-                    v.y = j + 1 < r ? v.y * s : 0.0f;
-                    v.z = j + 2 < r ? v.z * s : 0.0f;
-                    v.w = j + 3 < r ? v.w * s : 0.0f;
-                    *reinterpret_cast<float4 *>(&sm.u.h[off]) = v;
+                    *reinterpret_cast<float4 *>(&sm.h[off]) = v;
                 }
             }
             if (C > 1) { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); reading = true; }
             __syncthreads();
 
             // ---- step 2 -------------------------------------------------------------------------------------------
-            if (!live) continue;
             // terms of s h: ranks 32 b + 8 t + (0 .. 7) of a lane feed steps 2 b and 2 b + 1 (RK = 16: 4 t + (0 .. 3))
-            uint32_t ha[KS][4][TERMS];
+            uint32_t ha[TERMS][KS][4];
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
                 const int col = RK == 16 ? 4 * t : 32 * (k / 2) + 8 * t + 4 * (k & 1);
                 float4 va = make_float4(0.f, 0.f, 0.f, 0.f), vb = va;
-                if (col < (r + 15) / 16 * 16) {
-                    va = *reinterpret_cast<const float4 *>(&sm.u.h[ra * HSTR + col]);
-                    vb = *reinterpret_cast<const float4 *>(&sm.u.h[rb * HSTR + col]);
-                }
-                cut_pair<TERMS>(va.x, va.y, ha[k][0]);
-                cut_pair<TERMS>(vb.x, vb.y, ha[k][1]);
-                cut_pair<TERMS>(va.z, va.w, ha[k][2]);
-                cut_pair<TERMS>(vb.z, vb.w, ha[k][3]);
+                if (la) va = *reinterpret_cast<const float4 *>(&sm.h[ra * HSTR + col]);
+                if (lb) vb = *reinterpret_cast<const float4 *>(&sm.h[rb * HSTR + col]);
+                uint32_t c0[TERMS], c1[TERMS], c2[TERMS], c3[TERMS];
+                cut_pair<TERMS>(va.x, va.y, c0);
+                cut_pair<TERMS>(vb.x, vb.y, c1);
+                cut_pair<TERMS>(va.z, va.w, c2);
+                cut_pair<TERMS>(vb.z, vb.w, c3);
+#pragma unroll
+                for (int i = 0; i < TERMS; ++i) { ha[i][k][0] = c0[i]; ha[i][k][1] = c1[i]; ha[i][k][2] = c2[i]; ha[i][k][3] = c3[i]; }
             }
-            const uint16_t *brow = p.B[mat] + (size_t)a * N * p.rank_max;
-            const int nrow = 4 * (g >> 1) + (g & 1);                  // channel of a block that the lane's row of B is, + 2 for the second tile
-            for (int cb = cb0 + wk; cb < cb1; cb += wn) {
-                const size_t oa = (size_t)ta * N + cb * 16 + 4 * t, ob = (size_t)tb * N + cb * 16 + 4 * t;
-                float4 ya = make_float4(0.f, 0.f, 0.f, 0.f), yb = ya;
-                if constexpr (Y16) {
-                    if (base16) {
-                        uint2 qa = make_uint2(0u, 0u), qb = qa;
-                        if (la) qa = *reinterpret_cast<const uint2 *>(base16 + oa);
-                        if (lb) qb = *reinterpret_cast<const uint2 *>(base16 + ob);
-                        ya = make_float4(__uint_as_float(qa.x << 16), __uint_as_float(qa.x & 0xFFFF0000u),
-                                         __uint_as_float(qa.y << 16), __uint_as_float(qa.y & 0xFFFF0000u));
-                        yb = make_float4(__uint_as_float(qb.x << 16), __uint_as_float(qb.x & 0xFFFF0000u),
-                                         __uint_as_float(qb.y << 16), __uint_as_float(qb.y & 0xFFFF0000u));
-                    }
-                } else {
-                    if (base32) {
-                        if (la) ya = *reinterpret_cast<const float4 *>(base32 + oa);
-                        if (lb) yb = *reinterpret_cast<const float4 *>(base32 + ob);
-                    }
-                }
-                float d[2][4] = {};
+            // channel of a block that the lane's row of B is, + 2 for the second tile: a lane's results are 4 t .. 4 t + 3
+            const int nrow = 4 * (g >> 1) + (g & 1);
+            char *ya_at = y + ((size_t)(chunk + (la ? sm.perm[at + ra] : 0)) * N + ch0 + 4 * t) * E;
+            char *yb_at = y + ((size_t)(chunk + (lb ? sm.perm[at + rb] : 0)) * N + ch0 + 4 * t) * E;
+            int left = n_ch;                                          // channels from this stage on
+#pragma unroll 1
+            for (int q = 0; q < n2; ++q, left -= CH, ya_at += CH * E, yb_at += CH * E) {
+                const uint32_t st = arrive();
+                if (!live) continue;
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const uint16_t *b = brow + (size_t)(cb * 16 + nrow + 2 * j) * p.rank_max;
+                for (int b0 = 0; b0 < CH / 16; b0 += WN) {
+                    const int blk = b0 + wr;
+                    if (blk * 16 >= left) continue;
+                    uint32_t brow[2] = {st + (blk * 16 + nrow) * (RK * 2), st + (blk * 16 + nrow + 2) * (RK * 2)};
+                    float d[2][4] = {};
                     if constexpr (RK == 16) {
-                        uint2 w = make_uint2(0u, 0u);
-                        const int left = r - 4 * t;
-                        if (left > 0) w = *reinterpret_cast<const uint2 *>(b + 4 * t);
-                        if (left < 4) { w.x = keep2(w.x, left); w.y = keep2(w.y, left - 2); }
+                        const uint2 w0 = lora_lds64(brow[0] + 8 * t), w1 = lora_lds64(brow[1] + 8 * t);
 #pragma unroll
-                        for (int i = 0; i < TERMS; ++i)
-                            mma_bf16_16x8x16(d[j], ha[0][0][i], ha[0][1][i], ha[0][2][i], ha[0][3][i], w.x, w.y, d[j]);
-                    } else {
-                        uint4 w[RK / 32];
-#pragma unroll
-                        for (int k = 0; k < RK / 32; ++k) {
-                            const int left = r - 32 * k - 8 * t;
-                            w[k] = left > 0 ? *reinterpret_cast<const uint4 *>(b + 32 * k + 8 * t) : zero;
-                            if (left < 8) {
-                                w[k].x = keep2(w[k].x, left); w[k].y = keep2(w[k].y, left - 2);
-                                w[k].z = keep2(w[k].z, left - 4); w[k].w = keep2(w[k].w, left - 6);
-                            }
+                        for (int i = TERMS - 1; i >= 0; --i) {
+                            mma_bf16_16x8x16(d[0], ha[i][0][0], ha[i][0][1], ha[i][0][2], ha[i][0][3], w0.x, w0.y, d[0]);
+                            mma_bf16_16x8x16(d[1], ha[i][0][0], ha[i][0][1], ha[i][0][2], ha[i][0][3], w1.x, w1.y, d[1]);
                         }
+                    } else {
+                        uint4 w[2][RK / 32];
 #pragma unroll
-                        for (int k = 0; k < RK / 32; ++k) {
-                            if (32 * k >= r) continue;
+                        for (int k = 0; k < RK / 32; ++k)
 #pragma unroll
-                            for (int i = 0; i < TERMS; ++i) {
-                                mma_bf16_16x8x16(d[j], ha[2 * k][0][i], ha[2 * k][1][i], ha[2 * k][2][i], ha[2 * k][3][i],
-                                                 w[k].x, w[k].y, d[j]);
-                                mma_bf16_16x8x16(d[j], ha[2 * k + 1][0][i], ha[2 * k + 1][1][i], ha[2 * k + 1][2][i],
-                                                 ha[2 * k + 1][3][i], w[k].z, w[k].w, d[j]);
+                            for (int j = 0; j < 2; ++j) w[j][k] = lora_lds128(brow[j] + (((4 * k + t) ^ ((g & 1) * FB)) << 4));
+                        // the small terms first, so that the instruction's truncation of their sums is small too
+#pragma unroll
+                        for (int i = TERMS - 1; i >= 0; --i)
+#pragma unroll
+                            for (int k = 0; k < RK / 32; ++k) {
+#pragma unroll
+                                for (int j = 0; j < 2; ++j)
+                                    mma_bf16_16x8x16(d[j], ha[i][2 * k][0], ha[i][2 * k][1], ha[i][2 * k][2], ha[i][2 * k][3],
+                                                     w[j][k].x, w[j][k].y, d[j]);
+#pragma unroll
+                                for (int j = 0; j < 2; ++j)
+                                    mma_bf16_16x8x16(d[j], ha[i][2 * k + 1][0], ha[i][2 * k + 1][1], ha[i][2 * k + 1][2],
+                                                     ha[i][2 * k + 1][3], w[j][k].z, w[j][k].w, d[j]);
                             }
+                    }
+                    float4 ya = make_float4(d[0][0], d[0][1], d[1][0], d[1][1]), yb = make_float4(d[0][2], d[0][3], d[1][2], d[1][3]);
+                    if (base) {
+                        const uint32_t row_at = st + kBase + ra * (CH * E);
+                        if constexpr (Y16) {
+                            const uint2 qa = lora_lds64(row_at + blk * 32 + t * 8), qb = lora_lds64(row_at + 8 * CH * E + blk * 32 + t * 8);
+                            ya.x += __uint_as_float(qa.x << 16); ya.y += __uint_as_float(qa.x & 0xFFFF0000u);
+                            ya.z += __uint_as_float(qa.y << 16); ya.w += __uint_as_float(qa.y & 0xFFFF0000u);
+                            yb.x += __uint_as_float(qb.x << 16); yb.y += __uint_as_float(qb.x & 0xFFFF0000u);
+                            yb.z += __uint_as_float(qb.y << 16); yb.w += __uint_as_float(qb.y & 0xFFFF0000u);
+                        } else {
+                            const uint32_t col = ((blk * 4 + t) ^ ((g & 1) * FY)) << 4;
+                            const uint4 qa = lora_lds128(row_at + col), qb = lora_lds128(row_at + 8 * CH * E + col);
+                            ya.x += __uint_as_float(qa.x); ya.y += __uint_as_float(qa.y);
+                            ya.z += __uint_as_float(qa.z); ya.w += __uint_as_float(qa.w);
+                            yb.x += __uint_as_float(qb.x); yb.y += __uint_as_float(qb.y);
+                            yb.z += __uint_as_float(qb.z); yb.w += __uint_as_float(qb.w);
                         }
                     }
-                }
-                ya.x += d[0][0]; ya.y += d[0][1]; ya.z += d[1][0]; ya.w += d[1][1];
-                yb.x += d[0][2]; yb.y += d[0][3]; yb.z += d[1][2]; yb.w += d[1][3];
-                if constexpr (Y16) {
-                    auto pack = [](float4 v) {
-                        uint2 q;
-                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(q.x) : "f"(v.y), "f"(v.x));
-                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(q.y) : "f"(v.w), "f"(v.z));
-                        return q;
-                    };
-                    if (la) *reinterpret_cast<uint2 *>(y16 + oa) = pack(ya);
-                    if (lb) *reinterpret_cast<uint2 *>(y16 + ob) = pack(yb);
-                } else {
-                    if (la) *reinterpret_cast<float4 *>(y32 + oa) = ya;
-                    if (lb) *reinterpret_cast<float4 *>(y32 + ob) = yb;
+                    if constexpr (Y16) {
+                        auto pack = [](float4 v) {
+                            uint2 o;
+                            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o.x) : "f"(v.y), "f"(v.x));
+                            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o.y) : "f"(v.w), "f"(v.z));
+                            return o;
+                        };
+                        if (la) *reinterpret_cast<uint2 *>(ya_at + blk * 32) = pack(ya);
+                        if (lb) *reinterpret_cast<uint2 *>(yb_at + blk * 32) = pack(yb);
+                    } else {
+                        if (la) *reinterpret_cast<float4 *>(ya_at + blk * 64) = ya;
+                        if (lb) *reinterpret_cast<float4 *>(yb_at + blk * 64) = yb;
+                    }
                 }
             }
         }
         turn = (int)(((long long)turn + items) % clusters);
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     if (reading) cluster_wait();                                      // nobody leaves while its sums may be read
 }
 
-template <int RK, bool Y16>
-static cudaError_t launch_lora(LoraParams &p, int bound, cudaStream_t st) {
-    auto kernel = w2a8_lora_kernel<RK, Y16>;
-    constexpr size_t smem = sizeof(LoraSmem<RK>);
+template <int T, int RK, bool Y16>
+static cudaError_t launch_lora(LoraParams &p, cudaStream_t st) {
+    auto kernel = w2a8_lora_kernel<T, RK, Y16>;
+    constexpr size_t smem = sizeof(LoraSmem<LoraCfg<T, RK>>);
+    static_assert(smem * LoraCfg<T, RK>::kBlocksPerSm <= 226 * 1024, "does not fit an SM");
     static PerDeviceFlags configured;
     if (cudaError_t e = allow_dynamic_smem(kernel, configured, (int)smem)) return e;
     static PerDeviceTable<kLoraMaxCluster + 1> clusters;
@@ -432,10 +549,19 @@ static cudaError_t launch_lora(LoraParams &p, int bound, cudaStream_t st) {
     p.C = p.M <= 256 ? 8 : 4;
     const int forced = env_int("W2A8_LORA_C", 0);
     if (forced >= 1 && forced <= kLoraMaxCluster) p.C = forced;
-    (void)bound;
-    const int n = resident[p.C] > 0 ? resident[p.C] : 1;
+    // no more clusters than there can be items: tiles, matrices and the shares that pay
+    const int tiles = p.M / T + (p.M < p.adapters + 1 ? p.M : p.adapters + 1);
+    int n = resident[p.C] > 0 ? resident[p.C] : 1;
+    if ((long long)tiles * p.count * 8 < n) n = tiles * p.count * 8;
     return launch_kernel_clusters(kernel, dim3((unsigned)(n * p.C)), dim3(kLoraThreads), smem, st, pdl_enabled(),
                                   make_uint2((unsigned)p.C, 1u), p);
+}
+
+template <int RK>
+static cudaError_t launch_lora_rank(LoraParams &p, bool y16, cudaStream_t st) {
+    const int tile = env_int("W2A8_LORA_TILE", p.M <= 256 ? 16 : 64);
+    if (tile == 16) return y16 ? launch_lora<16, RK, true>(p, st) : launch_lora<16, RK, false>(p, st);
+    return y16 ? launch_lora<64, RK, true>(p, st) : launch_lora<64, RK, false>(p, st);
 }
 
 }  // namespace w2a8
@@ -486,13 +612,9 @@ extern "C" int w2a8_lora_grouped(const void *x_bf16, const int32_t *adapter, int
     p.adapter = adapter; p.rank = rank; p.scale = scale;
     p.count = count; p.adapters = adapters; p.rank_max = rank_max; p.M = M; p.K = K;
     cudaStream_t st = (cudaStream_t)stream;
-    auto go = [&](auto rk) {
-        constexpr int RK = decltype(rk)::value;
-        return y_is_bf16 ? launch_lora<RK, true>(p, 0, st) : launch_lora<RK, false>(p, 0, st);
-    };
-    const cudaError_t err = rank_max <= 16 ? go(std::integral_constant<int, 16>())
-                          : rank_max <= 32 ? go(std::integral_constant<int, 32>())
-                          : rank_max <= 64 ? go(std::integral_constant<int, 64>())
-                                           : go(std::integral_constant<int, 128>());
+    const cudaError_t err = rank_max <= 16 ? launch_lora_rank<16>(p, y_is_bf16, st)
+                          : rank_max <= 32 ? launch_lora_rank<32>(p, y_is_bf16, st)
+                          : rank_max <= 64 ? launch_lora_rank<64>(p, y_is_bf16, st)
+                                           : launch_lora_rank<128>(p, y_is_bf16, st);
     return err == cudaSuccess ? W2A8_OK : W2A8_ERR_CUDA;
 }
