@@ -10,9 +10,12 @@
 // 2^-26 of a turn) goes to sincospif.  Everything else is fp32, rounded once to the result's type.
 //
 // Bound: memory -- every value is read once and written once, about 3 (7 with the norm) operations per value.
-// A lane therefore owns V = 4 pairs of a row (two 16-byte loads of fp32), G lanes a row, so that the norm is a
-// shuffle inside G lanes; a CTA takes the rows of one token, whose sines and cosines it computes once, into shared
-// memory, while the loads of its first rows are on their way.
+// A lane therefore owns V pairs of a row in 16-byte accesses (V = 4 of fp32, 8 of bf16), G lanes a row, so that the norm
+// is a shuffle inside G lanes.  A group of lanes keeps its head and goes from token to token: addresses move on by one
+// addition, the norm's weights stay in registers, and the rows of the next tokens are on their way into slots of shared
+// memory of each thread (registers for them would cost the occupancy that keeps the memory busy).
+// The sines and cosines of the CTA's tokens are computed once, one per thread, into shared memory, while the first rows
+// are on their way.
 #include <math.h>
 
 #include "w2a8_common.cuh"
@@ -22,6 +25,7 @@ namespace w2a8 {
 constexpr int kRopeMaxTensors = 4;
 constexpr int kRopeMaxDim = 512;
 constexpr int kRopeMaxThreads = 320;
+constexpr int kRopeTurns = 1024;         // pairs of sine and cosine in shared memory: tokens of a CTA times pairs
 
 struct RopeTensor {
     const void *x;
@@ -32,8 +36,10 @@ struct RopeTensor {
 struct RopeParams {
     RopeTensor t[kRopeMaxTensors];
     int end[kRopeMaxTensors];        // rows (heads) of a token up to and with tensor i
-    int rows, rows_per_block;        // heads of a token in all / of them, per CTA
+    int rows, tokens_per_block;      // heads of a token in all; tokens of a CTA
+    int head_tiles;                  // CTAs that share a token's heads, next to each other in the grid
     int M, D, half;                  // half = rot / 2
+    float inv_D;
     int group_log2;                  // lanes of a row = 1 << group_log2
     int interleaved;
     const int32_t *pos;
@@ -41,37 +47,40 @@ struct RopeParams {
     float amp, eps;
 };
 
-// N consecutive values, N = 1, 4 or 8
-template <int N, bool B16>
-__device__ __forceinline__ void load_values(const void *base, long long at, float *v) {
-    if constexpr (B16) {
-        const uint16_t *p = reinterpret_cast<const uint16_t *>(base) + at;
-        uint32_t w[(N + 1) / 2];
-        if constexpr (N == 8) {
-            const uint4 q = *reinterpret_cast<const uint4 *>(p);
+// V consecutive values, copied ahead into a slot of shared memory that only this thread reads (single values: into a
+// register), and as fp32
+template <int V, bool B16>
+struct Piece {
+    static constexpr int kBytes = V * (B16 ? 2 : 4), kWords = (kBytes + 3) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const char *from) {
+        if constexpr (kBytes == 16) {
+            const uint4 q = *reinterpret_cast<const uint4 *>(from);
             w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
-        } else if constexpr (N == 4) {
-            const uint2 q = *reinterpret_cast<const uint2 *>(p);
+        } else if constexpr (kBytes == 8) {
+            const uint2 q = *reinterpret_cast<const uint2 *>(from);
             w[0] = q.x; w[1] = q.y;
+        } else if constexpr (B16) {
+            w[0] = *reinterpret_cast<const uint16_t *>(from);
         } else {
-            w[0] = *p;
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            v[i] = __uint_as_float((i & 1) ? (w[i / 2] & 0xFFFF0000u) : (w[i / 2] << 16));
-    } else {
-        const float *p = reinterpret_cast<const float *>(base) + at;
-        if constexpr (N == 1) {
-            v[0] = *p;
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; i += 4) {
-                const float4 q = *reinterpret_cast<const float4 *>(p + i);
-                v[i] = q.x; v[i + 1] = q.y; v[i + 2] = q.z; v[i + 3] = q.w;
-            }
+            w[0] = *reinterpret_cast<const uint32_t *>(from);
         }
     }
-}
+    static __device__ __forceinline__ void copy(uint32_t slot, const char *from) {
+        if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(slot), "l"(from) : "memory");
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(slot), "l"(from) : "memory");
+    }
+    __device__ __forceinline__ void read(uint32_t slot) {
+        if constexpr (kBytes == 16)
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(slot) : "memory");
+        else
+            asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(slot) : "memory");
+    }
+    __device__ __forceinline__ float value(int i) const {
+        if constexpr (B16) return __uint_as_float((i & 1) ? (w[i / 2] & 0xFFFF0000u) : (w[i / 2] << 16));
+        else return __uint_as_float(w[i]);
+    }
+};
 
 // two fp32 values to two bf16, to nearest, ties to even; `lo` goes to the low half
 __device__ __forceinline__ uint32_t to_bf16x2(float lo, float hi) {
@@ -84,13 +93,16 @@ template <int N, bool B16>
 __device__ __forceinline__ void store_values(void *base, long long at, const float *v) {
     if constexpr (B16) {
         uint16_t *p = reinterpret_cast<uint16_t *>(base) + at;
-        if constexpr (N == 8)
-            *reinterpret_cast<uint4 *>(p) = make_uint4(to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3]),
-                                                       to_bf16x2(v[4], v[5]), to_bf16x2(v[6], v[7]));
-        else if constexpr (N == 4)
+        if constexpr (N % 8 == 0) {
+#pragma unroll
+            for (int i = 0; i < N; i += 8)
+                *reinterpret_cast<uint4 *>(p + i) = make_uint4(to_bf16x2(v[i], v[i + 1]), to_bf16x2(v[i + 2], v[i + 3]),
+                                                               to_bf16x2(v[i + 4], v[i + 5]), to_bf16x2(v[i + 6], v[i + 7]));
+        } else if constexpr (N == 4) {
             *reinterpret_cast<uint2 *>(p) = make_uint2(to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3]));
-        else
+        } else {
             *p = (uint16_t)to_bf16x2(v[0], 0.0f);
+        }
     } else {
         float *p = reinterpret_cast<float *>(base) + at;
         if constexpr (N == 1) {
@@ -103,151 +115,197 @@ __device__ __forceinline__ void store_values(void *base, long long at, const flo
     }
 }
 
-// V pairs per lane and chunk, NC chunks per lane: V = 4 where sizes, strides and pointers allow vectors, else V = 1.
-template <int V, int NC, bool NORM, bool X16, bool O16>
-__global__ void __launch_bounds__(kRopeMaxThreads)
+// V pairs per lane and chunk, NC chunks per lane: V = 4 (8 where both sides allow it) where sizes, strides and pointers
+// allow vectors, else V = 1.
+template <int V, int NC, bool NORM, bool X16, bool O16, bool HALVES, bool DIRECT>
+__global__ void __launch_bounds__(kRopeMaxThreads, V * NC <= 8 && V > 1 ? 3 : 1)
 w2a8_rope_kernel(const RopeParams p) {
-    __shared__ float2 turn[kRopeMaxDim / 2];
+    constexpr int X = X16 ? 2 : 4;
+    using P = Piece<V, X16>;
+    // rows that are on their way: kRing slots of each thread
+    constexpr int kRing = DIRECT ? 1 : NC == 1 ? 4 : 2;
+    __shared__ __align__(16) float2 turn[kRopeTurns];
+    __shared__ __align__(16) char ring[DIRECT ? 16 : kRing * NC * 2 * P::kBytes * kRopeMaxThreads];
     pdl_launch_dependents();
     pdl_wait();                                      // the rows, and perhaps the positions, come from earlier kernels
-    const int token = blockIdx.x;
+    const int tile = blockIdx.x / p.head_tiles, head_tile = blockIdx.x - tile * p.head_tiles;
+    const int token0 = tile * p.tokens_per_block;
+    const int tokens = min(p.tokens_per_block, p.M - token0);
     const int G = 1 << p.group_log2;
-    const int lane = threadIdx.x & (G - 1), group = threadIdx.x >> p.group_log2;
-    const int groups = blockDim.x >> p.group_log2;
-    const int units = p.D / (2 * V);
-    const int row0 = blockIdx.y * p.rows_per_block;
-    const int row1 = min(p.rows, row0 + p.rows_per_block);
+    const int lane = threadIdx.x & (G - 1);
+    const int units = p.D / (2 * V), turned_units = p.half / V;
+    const int row = head_tile * (blockDim.x >> p.group_log2) + (threadIdx.x >> p.group_log2);
+    const bool live = row < p.rows;
 
-    float u[NC][V], v[NC][V];
-    const RopeTensor *t = nullptr;
-    int head = 0;
-    // the pairs of this lane: values (a + j, b + j) of the row, or 2V consecutive ones from 2 * pair on
-    auto load_row = [&](int row) {
-        int i = 0;
-        while (row >= p.end[i]) ++i;
-        t = &p.t[i];
-        head = row - (i ? p.end[i - 1] : 0);
-        const long long at = (long long)token * t->xt + (long long)head * t->xh;
+    int which = 0;
+    while (live && row >= p.end[which]) ++which;
+    const RopeTensor &t = p.t[which];
+    const int head = row - (which ? p.end[which - 1] : 0);
+    const char *src = static_cast<const char *>(t.x) + ((long long)token0 * t.xt + (long long)head * t.xh) * X;
+    char *dst = static_cast<char *>(t.out) + ((long long)token0 * t.ot + (long long)head * t.oh) * (O16 ? 2 : 4);
+    const long long src_step = t.xt * X, dst_step = t.ot * (O16 ? 2 : 4);
+
+    // The values of this lane in a row, two pieces of V each: (u, v) of pairs that lie `half` apart with HALVES, else 2V
+    // consecutive values, which are pairs of neighbours.  Those that are not rotated are any two pieces.
+    int off_a[NC], off_b[NC];
+    bool on[NC], turned[NC];
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int unit = c * G + lane;
+    for (int c = 0; c < NC; ++c) {
+        const int unit = c * G + lane;
+        on[c] = live && unit < units;
+        turned[c] = unit < turned_units;
+        const bool h = HALVES && turned[c];
+        off_a[c] = h ? unit * V : 2 * unit * V;
+        off_b[c] = h ? unit * V + p.half : 2 * unit * V + V;
+    }
+    const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring) + threadIdx.x * P::kBytes;
+    auto slot_of = [&](int slot, int c, int piece) { return mine + ((slot * NC + c) * 2 + piece) * (kRopeMaxThreads * P::kBytes); };
+    int ahead = 0;                                   // tokens whose rows have been asked for
+    auto ask = [&]() {
+        if constexpr (!DIRECT) {
+            if (ahead < tokens) {
+                const int slot = ahead % kRing;
 #pragma unroll
-            for (int j = 0; j < V; ++j) { u[c][j] = 0.0f; v[c][j] = 0.0f; }
-            if (unit >= units) continue;
-            const int pair = unit * V;
-            if (pair < p.half && !p.interleaved) {
-                load_values<V, X16>(t->x, at + pair, u[c]);
-                load_values<V, X16>(t->x, at + pair + p.half, v[c]);
-            } else if constexpr (V == 4) {
-                float e[8];
-                load_values<8, X16>(t->x, at + 2 * pair, e);
-#pragma unroll
-                for (int j = 0; j < V; ++j) { u[c][j] = e[2 * j]; v[c][j] = e[2 * j + 1]; }
-            } else {
-                load_values<1, X16>(t->x, at + 2 * pair, u[c]);
-                load_values<1, X16>(t->x, at + 2 * pair + 1, v[c]);
+                for (int c = 0; c < NC; ++c) {
+                    if (!on[c]) continue;
+                    P::copy(slot_of(slot, c, 0), src + off_a[c] * X);
+                    P::copy(slot_of(slot, c, 1), src + off_b[c] * X);
+                }
+                src += src_step;
+                ++ahead;
             }
+            asm volatile("cp.async.commit_group;" ::: "memory");
         }
     };
-
-    int row = row0 + group;
-    const bool first = row < row1;
-    if (first) load_row(row);
+    // DIRECT: rows go straight into registers, one token at a time
+    P now[NC][2];
+    auto load_row = [&]() {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            now[c][0] = now[c][1] = P{};
+            if (!on[c]) continue;
+            now[c][0].load(src + off_a[c] * X);
+            now[c][1].load(src + off_b[c] * X);
+        }
+        src += src_step;
+    };
+    if constexpr (DIRECT) {
+        load_row();
+    } else {
+#pragma unroll
+        for (int i = 0; i < kRing; ++i) ask();
+    }
     if (p.half > 0) {
-        const double t64 = (double)p.pos[token];
-        for (int i = threadIdx.x; i < p.half; i += blockDim.x) {
-            const double turns = t64 * (p.inv_freq[i] * 0.15915494309189533576888);     // 1 / (2 pi)
+        // One angle per thread.  The pairs of a token are stored by their place in a unit, then by unit: the lanes of a
+        // group read consecutive words.
+        for (int i = threadIdx.x; i < tokens * p.half; i += blockDim.x) {
+            const int tok = i / p.half, k = i - tok * p.half, pair = V == 1 ? k : k % turned_units * V + k / turned_units;
+            const double turns = (double)p.pos[token0 + tok] * (p.inv_freq[pair] * 0.15915494309189533576888);   // 1 / (2 pi)
             float s, c;
             sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
             turn[i] = make_float2(p.amp * c, p.amp * s);
         }
         __syncthreads();
     }
-    // every lane of a warp goes the same number of rounds, for the shuffles of the norm
-    for (int base = row0; base < row1; base += groups, row += groups) {
-        const bool live = row < row1;
-        if (base != row0 && live) load_row(row);
-        if constexpr (NORM) {
-            float sum = 0.0f;
-            if (live) {
+    float weight[NC][2 * V];                         // of the lane's values, for the norm
+    if constexpr (NORM) {
 #pragma unroll
-                for (int c = 0; c < NC; ++c)
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-                    for (int j = 0; j < V; ++j) sum = fmaf(u[c][j], u[c][j], fmaf(v[c][j], v[c][j], sum));
-            }
-            for (int o = G >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-            const float scale = 1.0f / sqrtf(sum / (float)p.D + p.eps);
+            for (int j = 0; j < 2 * V; ++j)
+                weight[c][j] = t.weight && on[c] ? t.weight[j < V ? off_a[c] + j : off_b[c] + j - V] : 1.0f;
+    }
+    const float2 *cs = turn + lane;
+#pragma unroll 1
+    for (int token = 0; token < tokens; ++token, cs += p.half, dst += dst_step) {
+        float e[NC][2 * V];                          // the lane's values: the two pieces
+        if constexpr (!DIRECT) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
-                for (int j = 0; j < V; ++j) { u[c][j] *= scale; v[c][j] *= scale; }
+                for (int k = 0; k < 2; ++k) now[c][k].read(slot_of(token % kRing, c, k));
         }
-        if (!live) continue;
-        const long long at = (long long)token * t->ot + (long long)head * t->oh;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int j = 0; j < V; ++j) { e[c][j] = now[c][0].value(j); e[c][V + j] = now[c][1].value(j); }
+        if constexpr (NORM) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                if (on[c]) {
+#pragma unroll
+                    for (int j = 0; j < 2 * V; ++j) sum = fmaf(e[c][j], e[c][j], sum);
+                }
+            for (int o = G >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+            const float scale = __frsqrt_rn(fmaf(sum, p.inv_D, p.eps));
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int j = 0; j < 2 * V; ++j) e[c][j] *= scale * weight[c][j];
+        }
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            const int unit = c * G + lane;
-            if (unit >= units) continue;
-            const int pair = unit * V;
-            const bool turned = pair < p.half, halves = turned && !p.interleaved;
-            if constexpr (NORM) {
-                if (t->weight) {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        u[c][j] *= t->weight[halves ? pair + j : 2 * (pair + j)];
-                        v[c][j] *= t->weight[halves ? pair + j + p.half : 2 * (pair + j) + 1];
-                    }
-                }
-            }
-            if (turned) {
+            if (!on[c]) continue;
+            if (turned[c]) {
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const float2 cs = turn[pair + j];
-                    const float a = u[c][j], b = v[c][j];
-                    u[c][j] = fmaf(a, cs.x, -(b * cs.y));
-                    v[c][j] = fmaf(b, cs.x, a * cs.y);
+                    const float2 q = cs[j * turned_units + c * G];
+                    float &u = HALVES ? e[c][j] : e[c][2 * j], &v = HALVES ? e[c][V + j] : e[c][2 * j + 1];
+                    const float x = u, y = v;
+                    u = fmaf(x, q.x, -(y * q.y));
+                    v = fmaf(y, q.x, x * q.y);
                 }
             }
-            if (halves) {
-                store_values<V, O16>(t->out, at + pair, u[c]);
-                store_values<V, O16>(t->out, at + pair + p.half, v[c]);
-            } else if constexpr (V == 4) {
-                float e[8];
-#pragma unroll
-                for (int j = 0; j < V; ++j) { e[2 * j] = u[c][j]; e[2 * j + 1] = v[c][j]; }
-                store_values<8, O16>(t->out, at + 2 * pair, e);
-            } else {
-                store_values<1, O16>(t->out, at + 2 * pair, u[c]);
-                store_values<1, O16>(t->out, at + 2 * pair + 1, v[c]);
-            }
+            store_values<V, O16>(dst, off_a[c], e[c]);
+            store_values<V, O16>(dst, off_b[c], e[c] + V);
         }
+        // the slot is free, or the registers are: the values have been used
+        if constexpr (!DIRECT) ask();
+        else if (token + 1 < tokens) load_row();
     }
 }
 
-template <int V, int NC, bool NORM>
+template <int V, int NC, bool NORM, bool HALVES, bool DIRECT>
 static cudaError_t launch_rope_types(const RopeParams &p, bool x16, bool o16, dim3 grid, int threads, cudaStream_t st) {
     auto go = [&](auto kernel) { return launch_kernel(kernel, grid, dim3(threads), 0, st, pdl_enabled(), p); };
-    if (x16) return o16 ? go(w2a8_rope_kernel<V, NC, NORM, true, true>) : go(w2a8_rope_kernel<V, NC, NORM, true, false>);
-    return o16 ? go(w2a8_rope_kernel<V, NC, NORM, false, true>) : go(w2a8_rope_kernel<V, NC, NORM, false, false>);
+    if (x16) return o16 ? go(w2a8_rope_kernel<V, NC, NORM, true, true, HALVES, DIRECT>) : go(w2a8_rope_kernel<V, NC, NORM, true, false, HALVES, DIRECT>);
+    if constexpr (V == 8) return cudaErrorNotSupported;       // 8 pairs per lane are for bf16 rows
+    else return o16 ? go(w2a8_rope_kernel<V, NC, NORM, false, true, HALVES, DIRECT>) : go(w2a8_rope_kernel<V, NC, NORM, false, false, HALVES, DIRECT>);
+}
+// A CTA of one token takes its rows straight into registers (one latency instead of two), and so do single values.
+template <int V, int NC, bool NORM>
+static cudaError_t launch_rope_layout(const RopeParams &p, bool x16, bool o16, dim3 grid, int threads, cudaStream_t st) {
+    if constexpr (V > 1)
+        if (p.tokens_per_block > 1)
+            return p.interleaved ? launch_rope_types<V, NC, NORM, false, false>(p, x16, o16, grid, threads, st)
+                                 : launch_rope_types<V, NC, NORM, true, false>(p, x16, o16, grid, threads, st);
+    return p.interleaved ? launch_rope_types<V, NC, NORM, false, true>(p, x16, o16, grid, threads, st)
+                         : launch_rope_types<V, NC, NORM, true, true>(p, x16, o16, grid, threads, st);
 }
 
+// vec: values, in rows and of the rotated part, that all sizes, strides and pointers are multiples of: 16, 8 or 1
 template <bool NORM>
-static cudaError_t launch_rope(RopeParams &p, bool vec, bool x16, bool o16, cudaStream_t st) {
-    const int units = p.D / (vec ? 8 : 2);
+static cudaError_t launch_rope(RopeParams &p, int vec, bool x16, bool o16, cudaStream_t st) {
+    const int V = vec == 16 && x16 ? 8 : vec >= 8 ? 4 : 1;
+    const int units = p.D / (2 * V);
     p.group_log2 = 0;
     while ((1 << p.group_log2) < units && p.group_log2 < 5) ++p.group_log2;
-    const int G = 1 << p.group_log2;
-    // rows of a token over CTAs of at most kRopeMaxThreads threads: one round each while there are few tokens
-    // (latency), all rows in as few CTAs as the rounds allow otherwise (sines and cosines once per token)
-    const int fit = kRopeMaxThreads / G;
-    p.rows_per_block = (long long)p.M * ((p.rows + fit - 1) / fit) <= 2 * sm_count() ? (p.rows < fit ? p.rows : fit) : p.rows;
-    const int rounds = (p.rows_per_block + fit - 1) / fit;
-    const int groups = (p.rows_per_block + rounds - 1) / rounds;
-    const int threads = (groups * G + 31) / 32 * 32;
-    const dim3 grid((unsigned)p.M, (unsigned)((p.rows + p.rows_per_block - 1) / p.rows_per_block));
-    if (!vec) return launch_rope_types<1, 8, NORM>(p, x16, o16, grid, threads, st);
-    return units <= 32 ? launch_rope_types<4, 1, NORM>(p, x16, o16, grid, threads, st)
-                       : launch_rope_types<4, 2, NORM>(p, x16, o16, grid, threads, st);
+    const int G = 1 << p.group_log2, fit = kRopeMaxThreads / G;
+    // heads over CTAs of at most kRopeMaxThreads threads; several tokens per CTA once these fill the device some times over
+    const int tiles = (p.rows + fit - 1) / fit, groups = (p.rows + tiles - 1) / tiles;
+    const int threads = (groups * G + 31) / 32 * 32, gy = (p.rows * G + threads - 1) / threads;
+    p.head_tiles = gy;
+    p.tokens_per_block = 1;
+    while (p.tokens_per_block < 8 && 2 * p.tokens_per_block * p.half <= kRopeTurns &&
+           (long long)p.M / (2 * p.tokens_per_block) * gy >= 8ll * sm_count())
+        p.tokens_per_block *= 2;
+    const dim3 grid((unsigned)((p.M + p.tokens_per_block - 1) / p.tokens_per_block) * gy);
+    if (V == 1) return launch_rope_layout<1, 8, NORM>(p, x16, o16, grid, threads, st);
+    if (V == 8) return launch_rope_layout<8, 1, NORM>(p, x16, o16, grid, threads, st);
+    return units <= 32 ? launch_rope_layout<4, 1, NORM>(p, x16, o16, grid, threads, st)
+                       : launch_rope_layout<4, 2, NORM>(p, x16, o16, grid, threads, st);
 }
 
 // Where the rows of a result lie, in bytes.
@@ -286,7 +344,7 @@ static int rope_common(bool norm, int count, const void *const *x, int x_is_bf16
     if (norm && !(eps >= 0.0f)) return W2A8_ERR_SHAPE;
     if (rot_dim > 0 && (!positions || !inv_freq)) return W2A8_ERR_NULL;
     RopeParams p = {};
-    bool vec = head_dim % 8 == 0 && rot_dim % 8 == 0;
+    int vec = head_dim % 16 == 0 && rot_dim % 16 == 0 ? 16 : head_dim % 8 == 0 && rot_dim % 8 == 0 ? 8 : 1;
     const int xe = x_is_bf16 ? 2 : 4, oe = out_is_bf16 ? 2 : 4;
     int rows = 0;
     RowSet in[kRopeMaxTensors], to[kRopeMaxTensors];
@@ -296,7 +354,7 @@ static int rope_common(bool norm, int count, const void *const *x, int x_is_bf16
         const long long ot = out_strides[2 * i], oh = out_strides[2 * i + 1];
         const int H = heads[i];
         constexpr long long kMax = 1ll << 40;
-        if (H < 1 || H > (1 << 20) || xt < 0 || xh < 0 || ot < 0 || oh < 0 || xt > kMax || xh > kMax || ot > kMax ||
+        if (H < 1 || H > (1 << 17) || xt < 0 || xh < 0 || ot < 0 || oh < 0 || xt > kMax || xh > kMax || ot > kMax ||
             oh > kMax)
             return W2A8_ERR_SHAPE;
         // rows of the result must not share elements: heads inside tokens, or tokens inside heads
@@ -307,11 +365,11 @@ static int rope_common(bool norm, int count, const void *const *x, int x_is_bf16
         if (norm && weight && weight[i] && (reinterpret_cast<uintptr_t>(weight[i]) & 3u)) return W2A8_ERR_ALIGN;
         in[i] = {static_cast<const char *>(x[i]), xt * xe, xh * xe, M, H, (long long)head_dim * xe};
         to[i] = {static_cast<const char *>(out[i]), ot * oe, oh * oe, M, H, (long long)head_dim * oe};
-        vec = vec && xt % 8 == 0 && xh % 8 == 0 && ot % 8 == 0 && oh % 8 == 0;
+        if (xt % 8 || xh % 8 || ot % 8 || oh % 8) vec = 1;       // 16 bytes of bf16
         p.t[i] = {x[i], out[i], norm && weight ? weight[i] : nullptr, xt, xh, ot, oh};
         rows += H;
         p.end[i] = rows;
-        if (rows > (1 << 21)) return W2A8_ERR_SHAPE;
+        if (rows > (1 << 17)) return W2A8_ERR_SHAPE;             // the grid's limit, at two rows per CTA and more
     }
     for (int i = 0; i < count; ++i)
         for (int j = 0; j < count; ++j) {
@@ -324,7 +382,7 @@ static int rope_common(bool norm, int count, const void *const *x, int x_is_bf16
     if ((reinterpret_cast<uintptr_t>(positions) & 3u) || (reinterpret_cast<uintptr_t>(inv_freq) & 7u)) return W2A8_ERR_ALIGN;
     if (int st = check_device()) return st;
     p.rows = rows;
-    p.M = M; p.D = head_dim; p.half = rot_dim / 2;
+    p.M = M; p.D = head_dim; p.inv_D = 1.0f / head_dim; p.half = rot_dim / 2;
     p.interleaved = interleaved != 0;
     p.pos = positions; p.inv_freq = inv_freq; p.amp = amplitude; p.eps = eps;
     const cudaError_t e = norm ? launch_rope<true>(p, vec, x_is_bf16, out_is_bf16, (cudaStream_t)stream)
