@@ -395,13 +395,18 @@ def _want(t: torch.Tensor, name: str, dtype, shape, device):
         raise ValueError(f"{name} must be contiguous")
 
 
-def _on_current_device(device, stream):
-    """The launch goes to the current device: tensors of another one are refused, and so is a stream of another."""
-    if device.type != "cuda":
+def _launch_stream(device, index, stream) -> int:
+    """Raw handle of the stream to launch on.  The launch goes to the current device: tensors of another one (`index`;
+    -1: not on a GPU) are refused, and so is a stream of another."""
+    if index < 0:
         raise ValueError(f"tensors are on {device}: a CUDA device is needed")
-    here = torch.cuda.current_device()
-    if device.index != here or (stream is not None and stream.device.index != here):
+    here = torch._C._cuda_getDevice()
+    if index != here or (stream is not None and stream.device.index != here):
         raise ValueError(f"tensors or stream are on another device than the current one (cuda:{here})")
+    return torch._C._cuda_getCurrentRawStream(here) if stream is None else int(stream.cuda_stream)
+
+
+_BF16, _F32, _F64, _I32 = torch.bfloat16, torch.float32, torch.float64, torch.int32
 
 
 class LoraGroup:
@@ -417,7 +422,7 @@ class LoraGroup:
             raise ValueError("A and B must be lists of one tensor per matrix")
         self.adapters, self.rank_max, self.K = (int(n) for n in self.A[0].shape)
         self.N = [int(b.shape[1]) for b in self.B]
-        self.device = self.A[0].device
+        self.device, self.index = self.A[0].device, self.A[0].get_device()
         for a, b, n in zip(self.A, self.B, self.N):
             _want(a, "A", torch.bfloat16, (self.adapters, self.rank_max, self.K), self.device)
             _want(b, "B", torch.bfloat16, (self.adapters, n, self.rank_max), self.device)
@@ -428,14 +433,18 @@ class LoraGroup:
         ptrs = ctypes.c_void_p * self.count
         self._a, self._b = ptrs(*[_ptr(t) for t in self.A]), ptrs(*[_ptr(t) for t in self.B])
         self._n = (ctypes.c_int * self.count)(*self.N)
+        self._rank, self._scale = _ptr(rank), _ptr(scale)
         self._ptrs = ptrs
 
-    def _outputs(self, name, tensors, M, dtype):
+    def _outputs(self, name, tensors, M, dtype, index):
         if len(tensors) != self.count:
             raise ValueError(f"{name} must have one tensor per matrix")
+        ptrs = []
         for t, n in zip(tensors, self.N):
-            _want(t, name, dtype, (M, n), self.device)
-        return self._ptrs(*[t.data_ptr() for t in tensors])
+            if t.dtype is not dtype or t.shape != (M, n) or t.get_device() != index or not t.is_contiguous():
+                _want(t, name, dtype, (M, n), self.device)
+            ptrs.append(t.data_ptr())
+        return self._ptrs(*ptrs)
 
 
 def w2a8_lora_grouped(x: torch.Tensor, adapter: torch.Tensor, lora: LoraGroup, base=None, y=None,
@@ -443,21 +452,25 @@ def w2a8_lora_grouped(x: torch.Tensor, adapter: torch.Tensor, lora: LoraGroup, b
     """y[i] = base[i] + the adapters of x's tokens on matrix i (adapter int32 [M]; outside [0, adapters): none), e.g.
     on the results of w2a8_linear_grouped.  base: list of [M][N_i] (fp32, or all bf16) or None = 0; y: list of outputs,
     may be `base` itself (in place), None: new ones.  See w2a8_lora_grouped in include/w2a8.h."""
-    M = int(x.shape[0])
-    _on_current_device(lora.device, stream)
-    _want(x, "x", torch.bfloat16, (M, lora.K), lora.device)
-    _want(adapter, "adapter", torch.int32, (M,), lora.device)
-    dtype = (base if base is not None else y)[0].dtype if base is not None or y is not None else out_dtype
-    if dtype not in (torch.float32, torch.bfloat16):
+    device, index = lora.device, lora.index
+    M = x.shape[0]
+    raw = _launch_stream(device, index, stream)
+    if x.dtype is not _BF16 or x.shape != (M, lora.K) or x.get_device() != index or not x.is_contiguous():
+        _want(x, "x", _BF16, (M, lora.K), device)
+    if adapter.dtype is not _I32 or adapter.shape != (M,) or adapter.get_device() != index or not adapter.is_contiguous():
+        _want(adapter, "adapter", _I32, (M,), device)
+    dtype = base[0].dtype if base is not None else y[0].dtype if y is not None else out_dtype
+    if dtype is not _F32 and dtype is not _BF16:
         raise TypeError("base and y must be float32 or bfloat16")
     if y is None:
-        y = [torch.empty((M, n), dtype=dtype, device=lora.device) for n in lora.N]
-    py = lora._outputs("y", y, M, dtype)
-    pb = None if base is None else py if base is y else lora._outputs("base", base, M, dtype)
-    _check(lib().w2a8_lora_grouped(x.data_ptr(), adapter.data_ptr(), lora.adapters, lora.rank_max, _ptr(lora.rank),
-                                   _ptr(lora.scale), lora.count, lora._a, lora._b, pb, py,
-                                   1 if dtype == torch.bfloat16 else 0, lora._n, M, lora.K, _stream(stream)),
-           "w2a8_lora_grouped")
+        y = [torch.empty((M, n), dtype=dtype, device=device) for n in lora.N]
+    py = lora._outputs("y", y, M, dtype, index)
+    pb = None if base is None else py if base is y else lora._outputs("base", base, M, dtype, index)
+    status = lib().w2a8_lora_grouped(x.data_ptr(), adapter.data_ptr(), lora.adapters, lora.rank_max, lora._rank,
+                                     lora._scale, lora.count, lora._a, lora._b, pb, py,
+                                     1 if dtype is _BF16 else 0, lora._n, M, lora.K, raw)
+    if status:
+        _check(status, "w2a8_lora_grouped")
     return y
 
 
@@ -490,7 +503,7 @@ class Heads:
         if not 1 <= self.count <= 4:
             raise ValueError("1 to 4 results")
         self.M, _, self.head_dim = (int(n) for n in self.x[0].shape)
-        self.device, self.dtype = self.x[0].device, self.x[0].dtype
+        self.device, self.index, self.dtype = self.x[0].device, self.x[0].get_device(), self.x[0].dtype
         if out is None:
             out = [torch.empty(t.shape, dtype=out_dtype or self.dtype, device=self.device) for t in self.x]
         self.out = list(out)
@@ -519,16 +532,18 @@ class Heads:
         self._xs = strides(*[t.stride(d) for t in self.x for d in (0, 1)])
         self._os = strides(*[t.stride(d) for t in self.out for d in (0, 1)])
         self._heads = (ctypes.c_int * self.count)(*[int(t.shape[1]) for t in self.x])
+        self._x16, self._o16 = int(self.dtype is torch.bfloat16), int(self.out_dtype is torch.bfloat16)
 
 
-def _rope_positions(heads: Heads, positions, inv_freq, stream):
-    _on_current_device(heads.device, stream)
-    if inv_freq is None:
-        return 0
-    rot = 2 * int(inv_freq.shape[0])
-    _want(inv_freq, "inv_freq", torch.float64, (rot // 2,), heads.device)
-    _want(positions, "positions", torch.int32, (heads.M,), heads.device)
-    return rot
+def _rope_angles(heads: Heads, positions, inv_freq) -> int:
+    """Checks positions and inv_freq; the number of values of a head that turn."""
+    half, index = inv_freq.shape[0], heads.index
+    if inv_freq.dtype is not _F64 or inv_freq.dim() != 1 or inv_freq.get_device() != index or not inv_freq.is_contiguous():
+        _want(inv_freq, "inv_freq", _F64, (half,), heads.device)
+    if (positions.dtype is not _I32 or positions.shape != (heads.M,) or positions.get_device() != index
+            or not positions.is_contiguous()):
+        _want(positions, "positions", _I32, (heads.M,), heads.device)
+    return 2 * half
 
 
 def w2a8_rope(heads: Heads, positions: torch.Tensor, inv_freq: torch.Tensor, amplitude: float = 1.0,
@@ -536,13 +551,13 @@ def w2a8_rope(heads: Heads, positions: torch.Tensor, inv_freq: torch.Tensor, amp
     """Rotary positions (int32 [M]) on the results of `heads`; the first 2 * len(inv_freq) values of a head turn.
     inv_freq (float64) and amplitude: from w2a8_rope_frequencies.  Returns heads.out.  See w2a8_rope in
     include/w2a8.h."""
-    if inv_freq is None:
-        raise TypeError("inv_freq must be a float64 tensor")
-    rot = _rope_positions(heads, positions, inv_freq, stream)
-    _check(lib().w2a8_rope(heads.count, heads._x, heads.dtype == torch.bfloat16, heads._out,
-                           heads.out_dtype == torch.bfloat16, heads._heads, heads._xs, heads._os, heads.M,
-                           heads.head_dim, rot, 1 if interleaved else 0, positions.data_ptr(), inv_freq.data_ptr(),
-                           amplitude, _stream(stream)), "w2a8_rope")
+    raw = _launch_stream(heads.device, heads.index, stream)
+    rot = _rope_angles(heads, positions, inv_freq)
+    status = lib().w2a8_rope(heads.count, heads._x, heads._x16, heads._out, heads._o16, heads._heads, heads._xs,
+                             heads._os, heads.M, heads.head_dim, rot, 1 if interleaved else 0, positions.data_ptr(),
+                             inv_freq.data_ptr(), amplitude, raw)
+    if status:
+        _check(status, "w2a8_rope")
     return heads.out
 
 
@@ -551,12 +566,14 @@ def w2a8_qk_norm_rope(heads: Heads, eps: float, positions: torch.Tensor | None =
                       stream=None):
     """The norm of every head (times heads.weight) and the rotation in one pass; without inv_freq the norm alone.
     Returns heads.out.  See w2a8_qk_norm_rope in include/w2a8.h."""
-    rot = _rope_positions(heads, positions, inv_freq, stream)
-    _check(lib().w2a8_qk_norm_rope(heads.count, heads._x, heads.dtype == torch.bfloat16, heads._out,
-                                   heads.out_dtype == torch.bfloat16, heads._w, eps, heads._heads, heads._xs,
-                                   heads._os, heads.M, heads.head_dim, rot, 1 if interleaved else 0,
-                                   _ptr(positions) if rot else 0, _ptr(inv_freq), amplitude, _stream(stream)),
-           "w2a8_qk_norm_rope")
+    raw = _launch_stream(heads.device, heads.index, stream)
+    rot = 0 if inv_freq is None else _rope_angles(heads, positions, inv_freq)
+    status = lib().w2a8_qk_norm_rope(heads.count, heads._x, heads._x16, heads._out, heads._o16, heads._w, eps,
+                                     heads._heads, heads._xs, heads._os, heads.M, heads.head_dim, rot,
+                                     1 if interleaved else 0, positions.data_ptr() if rot else None,
+                                     inv_freq.data_ptr() if rot else None, amplitude, raw)
+    if status:
+        _check(status, "w2a8_qk_norm_rope")
     return heads.out
 
 
