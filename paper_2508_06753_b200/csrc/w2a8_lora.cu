@@ -57,19 +57,18 @@ __device__ __forceinline__ void lora_copy16(uint32_t to, const void *from) {
 __device__ __forceinline__ void lora_copy_some(uint32_t to, const void *from, int bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ uint4 lora_lds128(uint32_t at) {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint2 lora_lds64(uint32_t at) {
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
-    return v;
+// D += A (16 x 16, bf16, row) * B (16 x 8, bf16, col), fp32; a pure function of its operands, so that the compiler may
+// put loads and other products between a chain of them.
+__device__ __forceinline__ void lora_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
 // An instance: tiles of T tokens, ranks of up to RK.  Everything that an address in the loops below depends on is a
-// constant of it.  Two CTAs per SM up to 64 ranks; with 128 the terms of s h need the registers of a whole SM.
+// constant of it.  One CTA per SM with large stages: two with half of the shared memory each were slower (32 tokens of 32
+// adapters of rank 64, gate|up of the 8B layer: 46 us, one 42; 16 tokens of one adapter 15 and 10), and the terms of s h
+// want the registers.
 template <int T_, int RK_>
 struct LoraCfg {
     static constexpr int T = T_, RK = RK_;
@@ -78,12 +77,11 @@ struct LoraCfg {
     static constexpr int NR = MT == 4 ? 2 : NT < 8 ? NT : 8;          // step 1: shares of the ranks among the warps
     static constexpr int NK = kLoraWarps / MT / NR;                   // and of K
     static constexpr int WN = kLoraWarps / MT;                        // step 2: shares of the channels
-    static constexpr int KC = T == 64 ? 64 : RK == 16 ? 256 : RK <= 64 ? 128 : 64;      // values of K per stage
-    static constexpr int CH = T == 64 ? (RK <= 64 ? 32 : 64) : 128;   // channels per stage
+    static constexpr int KC = T == 64 ? (RK <= 64 ? 128 : 64) : RK == 16 ? 512 : RK <= 64 ? 256 : 128;    // values of K per stage
+    static constexpr int CH = T == 64 ? (RK <= 64 ? 128 : 64) : RK <= 64 ? 256 : 128;   // channels per stage
     static constexpr int kBytes1 = (T + RK) * KC * 2, kBytes2 = CH * (2 * RK + 4 * T);
     static constexpr int kStageBytes = kBytes1 > kBytes2 ? kBytes1 : kBytes2;
-    static constexpr int kStages = 4;
-    static constexpr int kBlocksPerSm = RK <= 64 ? 2 : 1;
+    static constexpr int kStages = T == 64 && RK <= 64 ? 3 : 4;
     static constexpr int HSTR = RK + 4;          // floats between rows of h: no bank conflicts
 };
 template <typename Cfg>
@@ -191,8 +189,30 @@ __device__ __forceinline__ void lora_sort(LoraSmem<Cfg> &sm, const LoraParams &p
     __syncthreads();
 }
 
+// How the channels of the matrices are dealt out: in shares of `width` blocks of 16 at most, `total` of them for a tile.
+// A share does step 1 for itself, so shares cost; too few leave clusters idle in the last round.  The estimate of both, in
+// microseconds, is of measured rates of a CTA: 64 values of K in step 1, a block in step 2, and what an item takes beside.
+struct LoraShares { int width, total; float cost; };
+__host__ __device__ inline int lora_shares_of(int N, int width) { return (N / 16 + width - 1) / width; }
+constexpr int kLoraMaxShares = 16;       // of the widest matrix
+template <int T, int RK>
+__host__ __device__ inline LoraShares lora_shares(const LoraParams &p, int shares, int n_tiles, int clusters) {
+    constexpr float kUnit = T == 64 ? (RK <= 64 ? 0.45f : 0.72f) : RK <= 32 ? 0.14f : RK <= 64 ? 0.25f : 0.40f;
+    constexpr float kBlock = T == 64 ? (RK <= 64 ? 0.21f : 0.39f) : RK <= 32 ? 0.06f : RK <= 64 ? 0.10f : 0.16f;
+    constexpr float kItem = T == 64 ? 6.0f : 4.0f;
+    int widest = 0;
+    for (int i = 0; i < p.count; ++i) widest = p.N[i] > widest ? p.N[i] : widest;
+    LoraShares q;
+    q.width = (widest / 16 + shares - 1) / shares;
+    q.total = 0;
+    for (int i = 0; i < p.count; ++i) q.total += lora_shares_of(p.N[i], q.width);
+    const int rounds = (n_tiles * q.total + clusters - 1) / clusters;
+    q.cost = rounds * (kItem + (kUnit * (p.K / 64) + kBlock * q.width) / p.C);
+    return q;
+}
+
 template <int T, int RK, bool Y16>
-__global__ void __launch_bounds__(kLoraThreads, LoraCfg<T, RK>::kBlocksPerSm)
+__global__ void __launch_bounds__(kLoraThreads, 1)
 w2a8_lora_kernel(const LoraParams p) {
     using Cfg = LoraCfg<T, RK>;
     using Smem = LoraSmem<Cfg>;
@@ -209,6 +229,9 @@ w2a8_lora_kernel(const LoraParams p) {
     const int cluster = blockIdx.x / C, clusters = gridDim.x / C;
     const int L = p.adapters;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(sm.ring.stage[0]);
+    // reads of a stage, at byte offsets of the ring
+    auto lds128 = [&](uint32_t at) { return *reinterpret_cast<const uint4 *>(sm.ring.stage[0] + at); };
+    auto lds64 = [&](uint32_t at) { return *reinterpret_cast<const uint2 *>(sm.ring.stage[0] + at); };
     // Warps: MT tiles of 16 tokens, in step 1 times NR shares of the ranks and NK of K, in step 2 times WN of the channels.
     const int wm = warp % MT, wr = warp / MT, jr = wr % NR, jk = wr / NR;
     const int ra = wm * 16 + g, rb = ra + 8;                          // the lane's two tokens in the tile
@@ -243,22 +266,20 @@ w2a8_lora_kernel(const LoraParams p) {
 
         // ---- the items of the chunk, dealt to the clusters in turn -------------------------------------------------
         const int n_tiles = sm.tiles[L + 1];
-        const int whole = n_tiles * p.count;
-        // Few items: several clusters share the channels of one.  Each of them does step 1 for itself, so not many more
-        // than the bytes of step 2 are to those of step 1.
-        int shares = 1;
-        if (2 * whole <= clusters) {
-            int widest = 0;
-            for (int i = 0; i < p.count; ++i) widest = max(widest, p.N[i]);
-            const float toks = (float)min(Cfg::kChunk, p.M - chunk) / n_tiles;
-            const float s1 = (toks + p.rank_max) * p.K, s2 = widest * (p.rank_max + E * toks);
-            shares = min(clusters / whole, 1 + (int)min(2.0f * s2 / s1, 64.0f));
+        LoraShares parts = lora_shares<T, RK>(p, lane % kLoraMaxShares + 1, n_tiles, clusters);
+#pragma unroll
+        for (int o = kLoraMaxShares / 2; o > 0; o >>= 1) {           // the cheapest, of equal ones the widest
+            const float cost = __shfl_xor_sync(0xFFFFFFFFu, parts.cost, o);
+            const int width = __shfl_xor_sync(0xFFFFFFFFu, parts.width, o), total = __shfl_xor_sync(0xFFFFFFFFu, parts.total, o);
+            if (cost < parts.cost || (cost == parts.cost && width > parts.width)) parts = {width, total, cost};
         }
-        const int items = whole * shares;
+        const int items = n_tiles * parts.total;
         int item = cluster - turn;
         if (item < 0) item += clusters;
         for (; item < items; item += clusters) {
-            const int wi = item / shares, share = item - wi * shares, tile = wi / p.count, mat = wi - tile * p.count;
+            const int tile = item / parts.total;
+            int mat = 0, share = item - tile * parts.total;           // the tile's part: a share of a matrix's channels
+            while (share >= lora_shares_of(p.N[mat], parts.width)) share -= lora_shares_of(p.N[mat++], parts.width);
             int a = 0;                                                // adapter of the tile: the last with tiles[a] <= tile
             for (int step = 1 << (31 - __clz(L)); step > 0; step >>= 1)
                 if (a + step <= L && sm.tiles[a + step] <= tile) a += step;
@@ -269,8 +290,8 @@ w2a8_lora_kernel(const LoraParams p) {
             const char *base = static_cast<const char *>(p.base[mat]);
             char *y = static_cast<char *>(p.y[mat]);
             // blocks of 16 channels of this CTA
-            const int blocks = N / 16, parts = shares * C, part_id = share * C + crank;
-            const int per = blocks / parts, more = blocks - per * parts;
+            const int blocks = N / 16, n_parts = lora_shares_of(N, parts.width) * C, part_id = share * C + crank;
+            const int per = blocks / n_parts, more = blocks - per * n_parts;
             const int ch0 = (part_id * per + min(part_id, more)) * 16, n_ch = (per + (part_id < more)) * 16;
 
             if (r == 0) {                                             // nothing to add
@@ -343,7 +364,7 @@ w2a8_lora_kernel(const LoraParams p) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
                 __syncthreads();
                 issue();
-                const uint32_t st = ring + slot * STAGE;
+                const uint32_t st = slot * STAGE;
                 slot = slot + 1 == S ? 0 : slot + 1;
                 return st;
             };
@@ -367,17 +388,17 @@ w2a8_lora_kernel(const LoraParams p) {
                     const int b = b0 + jk;
                     if (KU > 1 && b >= k32) continue;
                     const uint32_t col = ((4 * b + t) ^ flip) << 4;
-                    const uint4 va = lora_lds128(xrow + col), vb = lora_lds128(xrow + 8 * KC * 2 + col);
+                    const uint4 va = lds128(xrow + col), vb = lds128(xrow + 8 * KC * 2 + col);
                     uint4 w[NTW];
 #pragma unroll
-                    for (int j = 0; j < NTW; ++j) w[j] = lora_lds128(arow + j * (8 * KC * 2) + col);
+                    for (int j = 0; j < NTW; ++j) w[j] = lds128(arow + j * (8 * KC * 2) + col);
                     // A sum of 32 products at a time joins the running one with a rounded addition: the instruction
                     // truncates where it aligns its addends, a bias that a long chain would add up.
                     float d[NTW][4] = {};
 #pragma unroll
-                    for (int j = 0; j < NTW; ++j) mma_bf16_16x8x16(d[j], va.x, vb.x, va.y, vb.y, w[j].x, w[j].y, d[j]);
+                    for (int j = 0; j < NTW; ++j) lora_mma(d[j], {va.x, vb.x, va.y, vb.y}, w[j].x, w[j].y);
 #pragma unroll
-                    for (int j = 0; j < NTW; ++j) mma_bf16_16x8x16(d[j], va.z, vb.z, va.w, vb.w, w[j].z, w[j].w, d[j]);
+                    for (int j = 0; j < NTW; ++j) lora_mma(d[j], {va.z, vb.z, va.w, vb.w}, w[j].z, w[j].w);
 #pragma unroll
                     for (int j = 0; j < NTW; ++j)
 #pragma unroll
@@ -463,47 +484,55 @@ w2a8_lora_kernel(const LoraParams p) {
                     const int blk = b0 + wr;
                     if (blk * 16 >= left) continue;
                     uint32_t brow[2] = {st + (blk * 16 + nrow) * (RK * 2), st + (blk * 16 + nrow + 2) * (RK * 2)};
-                    float d[2][4] = {};
+                    // One sum per term: chains of dependent products a third as long, and the small terms are added up among
+                    // themselves, so that the instruction's truncation of their sums is small too.
+                    float part[TERMS][2][4] = {};
                     if constexpr (RK == 16) {
-                        const uint2 w0 = lora_lds64(brow[0] + 8 * t), w1 = lora_lds64(brow[1] + 8 * t);
+                        const uint2 w0 = lds64(brow[0] + 8 * t), w1 = lds64(brow[1] + 8 * t);
 #pragma unroll
-                        for (int i = TERMS - 1; i >= 0; --i) {
-                            mma_bf16_16x8x16(d[0], ha[i][0][0], ha[i][0][1], ha[i][0][2], ha[i][0][3], w0.x, w0.y, d[0]);
-                            mma_bf16_16x8x16(d[1], ha[i][0][0], ha[i][0][1], ha[i][0][2], ha[i][0][3], w1.x, w1.y, d[1]);
+                        for (int i = 0; i < TERMS; ++i) {
+                            lora_mma(part[i][0], ha[i][0], w0.x, w0.y);
+                            lora_mma(part[i][1], ha[i][0], w1.x, w1.y);
                         }
                     } else {
                         uint4 w[2][RK / 32];
 #pragma unroll
                         for (int k = 0; k < RK / 32; ++k)
 #pragma unroll
-                            for (int j = 0; j < 2; ++j) w[j][k] = lora_lds128(brow[j] + (((4 * k + t) ^ ((g & 1) * FB)) << 4));
-                        // the small terms first, so that the instruction's truncation of their sums is small too
+                            for (int j = 0; j < 2; ++j) w[j][k] = lds128(brow[j] + (((4 * k + t) ^ ((g & 1) * FB)) << 4));
 #pragma unroll
-                        for (int i = TERMS - 1; i >= 0; --i)
+                        for (int k = 0; k < RK / 32; ++k) {
 #pragma unroll
-                            for (int k = 0; k < RK / 32; ++k) {
+                            for (int i = 0; i < TERMS; ++i)
 #pragma unroll
-                                for (int j = 0; j < 2; ++j)
-                                    mma_bf16_16x8x16(d[j], ha[i][2 * k][0], ha[i][2 * k][1], ha[i][2 * k][2], ha[i][2 * k][3],
-                                                     w[j][k].x, w[j][k].y, d[j]);
+                                for (int j = 0; j < 2; ++j) lora_mma(part[i][j], ha[i][2 * k], w[j][k].x, w[j][k].y);
 #pragma unroll
-                                for (int j = 0; j < 2; ++j)
-                                    mma_bf16_16x8x16(d[j], ha[i][2 * k + 1][0], ha[i][2 * k + 1][1], ha[i][2 * k + 1][2],
-                                                     ha[i][2 * k + 1][3], w[j][k].z, w[j][k].w, d[j]);
-                            }
+                            for (int i = 0; i < TERMS; ++i)
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) lora_mma(part[i][j], ha[i][2 * k + 1], w[j][k].z, w[j][k].w);
+                        }
                     }
+                    float d[2][4];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            d[j][c] = part[TERMS - 1][j][c];
+#pragma unroll
+                            for (int i = TERMS - 2; i >= 0; --i) d[j][c] += part[i][j][c];
+                        }
                     float4 ya = make_float4(d[0][0], d[0][1], d[1][0], d[1][1]), yb = make_float4(d[0][2], d[0][3], d[1][2], d[1][3]);
                     if (base) {
                         const uint32_t row_at = st + kBase + ra * (CH * E);
                         if constexpr (Y16) {
-                            const uint2 qa = lora_lds64(row_at + blk * 32 + t * 8), qb = lora_lds64(row_at + 8 * CH * E + blk * 32 + t * 8);
+                            const uint2 qa = lds64(row_at + blk * 32 + t * 8), qb = lds64(row_at + 8 * CH * E + blk * 32 + t * 8);
                             ya.x += __uint_as_float(qa.x << 16); ya.y += __uint_as_float(qa.x & 0xFFFF0000u);
                             ya.z += __uint_as_float(qa.y << 16); ya.w += __uint_as_float(qa.y & 0xFFFF0000u);
                             yb.x += __uint_as_float(qb.x << 16); yb.y += __uint_as_float(qb.x & 0xFFFF0000u);
                             yb.z += __uint_as_float(qb.y << 16); yb.w += __uint_as_float(qb.y & 0xFFFF0000u);
                         } else {
                             const uint32_t col = ((blk * 4 + t) ^ ((g & 1) * FY)) << 4;
-                            const uint4 qa = lora_lds128(row_at + col), qb = lora_lds128(row_at + 8 * CH * E + col);
+                            const uint4 qa = lds128(row_at + col), qb = lds128(row_at + 8 * CH * E + col);
                             ya.x += __uint_as_float(qa.x); ya.y += __uint_as_float(qa.y);
                             ya.z += __uint_as_float(qa.z); ya.w += __uint_as_float(qa.w);
                             yb.x += __uint_as_float(qb.x); yb.y += __uint_as_float(qb.y);
@@ -536,7 +565,7 @@ template <int T, int RK, bool Y16>
 static cudaError_t launch_lora(LoraParams &p, cudaStream_t st) {
     auto kernel = w2a8_lora_kernel<T, RK, Y16>;
     constexpr size_t smem = sizeof(LoraSmem<LoraCfg<T, RK>>);
-    static_assert(smem * LoraCfg<T, RK>::kBlocksPerSm <= 226 * 1024, "does not fit an SM");
+    static_assert(smem <= 227 * 1024, "does not fit an SM");
     static PerDeviceFlags configured;
     if (cudaError_t e = allow_dynamic_smem(kernel, configured, (int)smem)) return e;
     static PerDeviceTable<kLoraMaxCluster + 1> clusters;
@@ -546,20 +575,37 @@ static cudaError_t launch_lora(LoraParams &p, cudaStream_t st) {
             n[C] = found > 0 ? found : sm_count() / C;
         }
     });
-    p.C = p.M <= 256 ? 8 : 4;
+    // The cluster size by the estimate above, for tokens that are evenly spread over the adapters; the number of clusters
+    // for as many tiles as there may be (tokens without an adapter can be one more).
+    const int used = p.M < p.adapters ? p.M : p.adapters;
+    const int tiles = used * (int)((p.M + (long long)used * T - 1) / ((long long)used * T)), bound = p.M / T + used + 1;
     const int forced = env_int("W2A8_LORA_C", 0);
-    if (forced >= 1 && forced <= kLoraMaxCluster) p.C = forced;
-    // no more clusters than there can be items: tiles, matrices and the shares that pay
-    const int tiles = p.M / T + (p.M < p.adapters + 1 ? p.M : p.adapters + 1);
-    int n = resident[p.C] > 0 ? resident[p.C] : 1;
-    if ((long long)tiles * p.count * 8 < n) n = tiles * p.count * 8;
+    int C = 0, n = 0;
+    float cost = 0.0f;
+    for (int c = 1; c <= kLoraMaxCluster; c = forced >= 1 && forced <= kLoraMaxCluster ? c + 1 : 2 * c) {
+        if (forced >= 1 && forced <= kLoraMaxCluster && c != forced) continue;
+        p.C = c;
+        int most = 0;                                            // shares of a tile that there can be
+        float best = 0.0f;
+        for (int sh = 1; sh <= kLoraMaxShares; ++sh) {
+            const LoraShares q = lora_shares<T, RK>(p, sh, tiles, resident[c]);
+            if (sh == 1 || q.cost < best) best = q.cost;
+            most = q.total > most ? q.total : most;
+        }
+        if (C && best >= cost) continue;
+        C = c; cost = best;
+        n = (long long)bound * most < resident[c] ? bound * most : resident[c];
+    }
+    p.C = C;
     return launch_kernel_clusters(kernel, dim3((unsigned)(n * p.C)), dim3(kLoraThreads), smem, st, pdl_enabled(),
                                   make_uint2((unsigned)p.C, 1u), p);
 }
 
 template <int RK>
 static cudaError_t launch_lora_rank(LoraParams &p, bool y16, cudaStream_t st) {
-    const int tile = env_int("W2A8_LORA_TILE", p.M <= 256 ? 16 : 64);
+    // Tiles of 16 tokens for decode batches: few tokens, or many adapters for the tokens (at 256 tokens of 64 adapters of
+    // rank 64 tiles of 64 take 209 us, of 16 76; with one adapter 29 and 26; at 1024 tokens of 4 adapters 56 and 73).
+    const int tile = env_int("W2A8_LORA_TILE", p.M <= 256 || p.M <= 4 * p.adapters ? 16 : 64);
     if (tile == 16) return y16 ? launch_lora<16, RK, true>(p, st) : launch_lora<16, RK, false>(p, st);
     return y16 ? launch_lora<64, RK, true>(p, st) : launch_lora<64, RK, false>(p, st);
 }
