@@ -53,6 +53,11 @@ __device__ __forceinline__ float4 lora_ld_cluster(uint32_t local, uint32_t rank)
 __device__ __forceinline__ void lora_copy16(uint32_t to, const void *from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
+// the same, or zeros
+__device__ __forceinline__ void lora_copy16_or_zero(uint32_t to, const void *from, bool zero) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\tcp.async.cg.shared.global [%0], [%1], 16, p;\n\t}"
+                 ::"r"(to), "l"(from), "r"((uint32_t)zero) : "memory");
+}
 // the first `bytes` of 16, zeros behind them
 __device__ __forceinline__ void lora_copy_some(uint32_t to, const void *from, int bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
@@ -319,32 +324,24 @@ w2a8_lora_kernel(const LoraParams p) {
                 src_y[i] = base + ((size_t)(chunk + sm.perm[at + row]) * N + ch0) * E + cy * 16;
             }
             const char *src_a = reinterpret_cast<const char *>(p.A[mat] + ((size_t)a * p.rank_max + rx) * p.K + u0 * 64 + cx * 8);
-            // the bytes of a piece of B that are ranks of the adapter: the rest counts as zero, whatever the row holds
+            // Ranks of B behind the adapter's last, up to the end of a step of 32 (16), count as zero, whatever the row holds:
+            // of a piece, b_bytes are the adapter's.
             const int b_bytes = min(max(r - cb * 8, 0), 8) * 2;
-            const char *src_b = reinterpret_cast<const char *>(p.B[mat] + ((size_t)a * N + ch0 + rbb) * p.rank_max + (b_bytes ? cb * 8 : 0));
+            const bool b_zero = b_bytes == 0, b_piece = cb * 8 < (RK == 16 ? 16 : (r + 31) / 32 * 32);
+            const char *src_b = reinterpret_cast<const char *>(p.B[mat] + ((size_t)a * N + ch0 + rbb) * p.rank_max + (b_zero ? 0 : cb * 8));
+            const int b_step = DB * p.rank_max * 2, a_step = DX * p.K * 2;
             int q_issue = 0, slot_issue = 0;
-            auto issue = [&]() {
+            auto issue2 = [&]() {                                     // a stage of step 2
                 const uint32_t st = ring + slot_issue * STAGE;
-                if (q_issue < n1) {
-                    if (KU == 1 || cx < (n_units - q_issue * KU) * 8) {
+                const int cw = n_ch - (q_issue - n1) * CH;            // channels that are left
+                if (cw > 0) {
+                    if (b_piece) {
+                        const char *src = src_b;
 #pragma unroll
-                        for (int i = 0; i < PX; ++i)
-                            if (T % DX == 0 || rx + i * DX < T)
-                                lora_copy_some(st + to_x + i * (kLoraThreads * 16), src_x[i], rx + i * DX < n ? 16 : 0);
-#pragma unroll
-                        for (int i = 0; i < PA; ++i)
-                            if (rx + i * DX < r)
-                                lora_copy16(st + kA + to_x + i * (kLoraThreads * 16), src_a + (size_t)(i * DX) * p.K * 2);
+                        for (int i = 0; i < PB; ++i, src += b_step)
+                            if (rbb + i * DB < cw && (CH % DB == 0 || rbb + i * DB < CH))
+                                lora_copy_some(st + to_b + i * (kLoraThreads * 16), src, b_bytes);
                     }
-#pragma unroll
-                    for (int i = 0; i < PX; ++i) src_x[i] += KC * 2;
-                    src_a += KC * 2;
-                } else if (q_issue < n1 + n2) {
-                    const int cw = n_ch - (q_issue - n1) * CH;        // channels that are left
-#pragma unroll
-                    for (int i = 0; i < PB; ++i)
-                        if (rbb + i * DB < min(cw, CH))
-                            lora_copy_some(st + to_b + i * (kLoraThreads * 16), src_b + (size_t)(i * DB) * p.rank_max * 2, b_bytes);
                     src_b += (size_t)CH * p.rank_max * 2;
                     if (base && cy * (16 / E) < cw) {
 #pragma unroll
@@ -358,12 +355,32 @@ w2a8_lora_kernel(const LoraParams p) {
                 ++q_issue;
                 slot_issue = slot_issue + 1 == S ? 0 : slot_issue + 1;
             };
+            auto issue = [&]() {
+                if (q_issue >= n1) { issue2(); return; }
+                const uint32_t st = ring + slot_issue * STAGE;
+                if (KU == 1 || cx < (n_units - q_issue * KU) * 8) {
+#pragma unroll
+                    for (int i = 0; i < PX; ++i)
+                        if (T % DX == 0 || rx + i * DX < T)
+                            lora_copy16_or_zero(st + to_x + i * (kLoraThreads * 16), src_x[i], rx + i * DX >= n);
+                    const char *src = src_a;
+#pragma unroll
+                    for (int i = 0; i < PA; ++i, src += a_step)
+                        if (rx + i * DX < r) lora_copy16(st + kA + to_x + i * (kLoraThreads * 16), src);
+                }
+#pragma unroll
+                for (int i = 0; i < PX; ++i) src_x[i] += KC * 2;
+                src_a += KC * 2;
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                ++q_issue;
+                slot_issue = slot_issue + 1 == S ? 0 : slot_issue + 1;
+            };
             // every stage is one group, also an empty one: S - 2 groups may still be open when a stage is needed
             int slot = 0;
-            auto arrive = [&]() {
+            auto arrive = [&](auto &&next) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
                 __syncthreads();
-                issue();
+                next();
                 const uint32_t st = slot * STAGE;
                 slot = slot + 1 == S ? 0 : slot + 1;
                 return st;
@@ -379,7 +396,7 @@ w2a8_lora_kernel(const LoraParams p) {
             const uint32_t flip = (g & 1) << 2;
 #pragma unroll 1
             for (int q = 0; q < n1; ++q) {
-                const uint32_t st = arrive();
+                const uint32_t st = arrive(issue);
                 if (!live) continue;
                 const uint32_t xrow = st + ra * (KC * 2), arow = st + kA + (jr * NTW * 8 + g) * (KC * 2);
                 const int k32 = KU == 1 ? 2 : 2 * (n_units - q * KU);
@@ -477,7 +494,7 @@ w2a8_lora_kernel(const LoraParams p) {
             int left = n_ch;                                          // channels from this stage on
 #pragma unroll 1
             for (int q = 0; q < n2; ++q, left -= CH, ya_at += CH * E, yb_at += CH * E) {
-                const uint32_t st = arrive();
+                const uint32_t st = arrive(issue2);
                 if (!live) continue;
 #pragma unroll
                 for (int b0 = 0; b0 < CH / 16; b0 += WN) {
@@ -502,6 +519,7 @@ w2a8_lora_kernel(const LoraParams p) {
                             for (int j = 0; j < 2; ++j) w[j][k] = lds128(brow[j] + (((4 * k + t) ^ ((g & 1) * FB)) << 4));
 #pragma unroll
                         for (int k = 0; k < RK / 32; ++k) {
+                            if (k > 0 && 32 * k >= r) break;
 #pragma unroll
                             for (int i = 0; i < TERMS; ++i)
 #pragma unroll
