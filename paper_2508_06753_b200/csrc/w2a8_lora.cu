@@ -40,6 +40,7 @@ struct LoraParams {
     void *y[kLoraMaxMatrices];
     int N[kLoraMaxMatrices];
     int count, adapters, rank_max, M, K, C;
+    int tiles_guess, width_guess;        // the host's: width of a share (below) for that many tiles
 };
 
 __device__ __forceinline__ float4 lora_ld_cluster(uint32_t local, uint32_t rank) {
@@ -271,12 +272,19 @@ w2a8_lora_kernel(const LoraParams p) {
 
         // ---- the items of the chunk, dealt to the clusters in turn -------------------------------------------------
         const int n_tiles = sm.tiles[L + 1];
-        LoraShares parts = lora_shares<T, RK>(p, lane % kLoraMaxShares + 1, n_tiles, clusters);
+        LoraShares parts;
+        if (n_tiles == p.tiles_guess) {
+            parts.width = p.width_guess;
+            parts.total = 0;
+            for (int i = 0; i < p.count; ++i) parts.total += lora_shares_of(p.N[i], parts.width);
+        } else {
+            parts = lora_shares<T, RK>(p, lane % kLoraMaxShares + 1, n_tiles, clusters);
 #pragma unroll
-        for (int o = kLoraMaxShares / 2; o > 0; o >>= 1) {           // the cheapest, of equal ones the widest
-            const float cost = __shfl_xor_sync(0xFFFFFFFFu, parts.cost, o);
-            const int width = __shfl_xor_sync(0xFFFFFFFFu, parts.width, o), total = __shfl_xor_sync(0xFFFFFFFFu, parts.total, o);
-            if (cost < parts.cost || (cost == parts.cost && width > parts.width)) parts = {width, total, cost};
+            for (int o = kLoraMaxShares / 2; o > 0; o >>= 1) {       // the cheapest, of equal ones the widest
+                const float cost = __shfl_xor_sync(0xFFFFFFFFu, parts.cost, o);
+                const int width = __shfl_xor_sync(0xFFFFFFFFu, parts.width, o), total = __shfl_xor_sync(0xFFFFFFFFu, parts.total, o);
+                if (cost < parts.cost || (cost == parts.cost && width > parts.width)) parts = {width, total, cost};
+            }
         }
         const int items = n_tiles * parts.total;
         int item = cluster - turn;
@@ -593,28 +601,30 @@ static cudaError_t launch_lora(LoraParams &p, cudaStream_t st) {
             n[C] = found > 0 ? found : sm_count() / C;
         }
     });
-    // The cluster size by the estimate above, for tokens that are evenly spread over the adapters; the number of clusters
-    // for as many tiles as there may be (tokens without an adapter can be one more).
-    const int used = p.M < p.adapters ? p.M : p.adapters;
-    const int tiles = used * (int)((p.M + (long long)used * T - 1) / ((long long)used * T)), bound = p.M / T + used + 1;
+    // The cluster size by the estimate above, for a guess of the tiles: one per adapter, and the full ones where there are
+    // many tokens.  The number of clusters for as many tiles as there may be (tokens without an adapter can be one more).
+    const int used = p.M < p.adapters ? p.M : p.adapters, bound = p.M / T + used + 1;
+    const int tiles = p.M <= (long long)used * T ? used : p.M / T + used;
     const int forced = env_int("W2A8_LORA_C", 0);
+    const bool force = forced >= 1 && forced <= kLoraMaxCluster;
     int C = 0, n = 0;
-    float cost = 0.0f;
-    for (int c = 1; c <= kLoraMaxCluster; c = forced >= 1 && forced <= kLoraMaxCluster ? c + 1 : 2 * c) {
-        if (forced >= 1 && forced <= kLoraMaxCluster && c != forced) continue;
+    LoraShares cheapest = {};
+    for (int c = force ? forced : 1; c <= (force ? forced : kLoraMaxCluster); c *= 2) {
         p.C = c;
         int most = 0;                                            // shares of a tile that there can be
-        float best = 0.0f;
+        LoraShares best = {};
         for (int sh = 1; sh <= kLoraMaxShares; ++sh) {
             const LoraShares q = lora_shares<T, RK>(p, sh, tiles, resident[c]);
-            if (sh == 1 || q.cost < best) best = q.cost;
+            if (sh == 1 || q.cost < best.cost) best = q;
             most = q.total > most ? q.total : most;
         }
-        if (C && best >= cost) continue;
-        C = c; cost = best;
+        if (C && best.cost >= cheapest.cost) continue;
+        C = c; cheapest = best;
         n = (long long)bound * most < resident[c] ? bound * most : resident[c];
     }
     p.C = C;
+    p.tiles_guess = n == resident[C] ? tiles : 0;                // the estimate is for all clusters that fit
+    p.width_guess = cheapest.width;
     return launch_kernel_clusters(kernel, dim3((unsigned)(n * p.C)), dim3(kLoraThreads), smem, st, pdl_enabled(),
                                   make_uint2((unsigned)p.C, 1u), p);
 }
