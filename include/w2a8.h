@@ -416,8 +416,8 @@ int w2a8_linear_grouped_host(const void *x_host, int M, int K, int count, const 
  *            Otherwise y[i] overlaps neither x, base nor another y
  *            (W2A8_ERR_SHAPE).
  *   N        HOST array of `count` entries
- * 1 <= adapters <= 1024, rank_max a multiple of 8 up to 128, M, N and K as
- * elsewhere.  One launch, no workspace: the tokens are sorted by adapter inside
+ * 1 <= adapters <= 1024, rank_max a multiple of 8 up to 128, M (up to 2^30), N
+ * and K as elsewhere.  One launch, no workspace: the tokens are sorted by adapter inside
  * it.  Repeated calls give equal bits, and a token's result does not depend on
  * the other tokens' values.  The adapters are read after the previous kernel of
  * the stream has completed, so they may be exchanged between calls.

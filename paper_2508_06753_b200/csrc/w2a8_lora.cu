@@ -649,7 +649,7 @@ extern "C" int w2a8_lora_grouped(const void *x_bf16, const int32_t *adapter, int
     EnvScope scope;
     if (!x_bf16 || !adapter || !A || !B || !y || !N) return W2A8_ERR_NULL;
     if (count < 1 || count > kLoraMaxMatrices || adapters < 1 || adapters > kLoraMaxAdapters || rank_max < 8 ||
-        rank_max > kLoraMaxRank || rank_max % 8)
+        rank_max > kLoraMaxRank || rank_max % 8 || M > (1 << 30))      // tokens are counted in 32 bits, a chunk ahead
         return W2A8_ERR_SHAPE;
     LoraParams p = {};
     const size_t e = y_is_bf16 ? 2 : 4;
