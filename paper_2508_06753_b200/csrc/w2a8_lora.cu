@@ -499,86 +499,91 @@ w2a8_lora_kernel(const LoraParams p) {
             const int nrow = 4 * (g >> 1) + (g & 1);
             char *ya_at = y + ((size_t)(chunk + (la ? sm.perm[at + ra] : 0)) * N + ch0 + 4 * t) * E;
             char *yb_at = y + ((size_t)(chunk + (lb ? sm.perm[at + rb] : 0)) * N + ch0 + 4 * t) * E;
-            int left = n_ch;                                          // channels from this stage on
-#pragma unroll 1
-            for (int q = 0; q < n2; ++q, left -= CH, ya_at += CH * E, yb_at += CH * E) {
-                const uint32_t st = arrive(issue2);
-                if (!live) continue;
+            // 16 channels of the stage at byte `st` for the lane's 16 tokens: tokens are the rows of mma.sync, channels its columns
+            auto block = [&](uint32_t st, int blk) {
+                const uint32_t brow[2] = {st + (blk * 16 + nrow) * (RK * 2), st + (blk * 16 + nrow + 2) * (RK * 2)};
+                // One sum per term: short chains of dependent products, and the small terms are added up among themselves,
+                // so that the instruction's truncation of their sums is small too.
+                float part[TERMS][2][4] = {};
+                if constexpr (RK == 16) {
+                    const uint2 w0 = lds64(brow[0] + 8 * t), w1 = lds64(brow[1] + 8 * t);
 #pragma unroll
-                for (int b0 = 0; b0 < CH / 16; b0 += WN) {
-                    const int blk = b0 + wr;
-                    if (blk * 16 >= left) continue;
-                    uint32_t brow[2] = {st + (blk * 16 + nrow) * (RK * 2), st + (blk * 16 + nrow + 2) * (RK * 2)};
-                    // One sum per term: chains of dependent products a third as long, and the small terms are added up among
-                    // themselves, so that the instruction's truncation of their sums is small too.
-                    float part[TERMS][2][4] = {};
-                    if constexpr (RK == 16) {
-                        const uint2 w0 = lds64(brow[0] + 8 * t), w1 = lds64(brow[1] + 8 * t);
-#pragma unroll
-                        for (int i = 0; i < TERMS; ++i) {
-                            lora_mma(part[i][0], ha[i][0], w0.x, w0.y);
-                            lora_mma(part[i][1], ha[i][0], w1.x, w1.y);
-                        }
-                    } else {
-                        uint4 w[2][RK / 32];
-#pragma unroll
-                        for (int k = 0; k < RK / 32; ++k)
-#pragma unroll
-                            for (int j = 0; j < 2; ++j) w[j][k] = lds128(brow[j] + (((4 * k + t) ^ ((g & 1) * FB)) << 4));
-#pragma unroll
-                        for (int k = 0; k < RK / 32; ++k) {
-                            if (k > 0 && 32 * k >= r) break;
-#pragma unroll
-                            for (int i = 0; i < TERMS; ++i)
-#pragma unroll
-                                for (int j = 0; j < 2; ++j) lora_mma(part[i][j], ha[i][2 * k], w[j][k].x, w[j][k].y);
-#pragma unroll
-                            for (int i = 0; i < TERMS; ++i)
-#pragma unroll
-                                for (int j = 0; j < 2; ++j) lora_mma(part[i][j], ha[i][2 * k + 1], w[j][k].z, w[j][k].w);
-                        }
+                    for (int i = 0; i < TERMS; ++i) {
+                        lora_mma(part[i][0], ha[i][0], w0.x, w0.y);
+                        lora_mma(part[i][1], ha[i][0], w1.x, w1.y);
                     }
-                    float d[2][4];
+                } else {
+                    uint4 w[2][RK / 32];
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
+                    for (int k = 0; k < RK / 32; ++k)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            d[j][c] = part[TERMS - 1][j][c];
+                        for (int j = 0; j < 2; ++j) w[j][k] = lds128(brow[j] + (((4 * k + t) ^ ((g & 1) * FB)) << 4));
 #pragma unroll
-                            for (int i = TERMS - 2; i >= 0; --i) d[j][c] += part[i][j][c];
-                        }
-                    float4 ya = make_float4(d[0][0], d[0][1], d[1][0], d[1][1]), yb = make_float4(d[0][2], d[0][3], d[1][2], d[1][3]);
-                    if (base) {
-                        const uint32_t row_at = st + kBase + ra * (CH * E);
-                        if constexpr (Y16) {
-                            const uint2 qa = lds64(row_at + blk * 32 + t * 8), qb = lds64(row_at + 8 * CH * E + blk * 32 + t * 8);
-                            ya.x += __uint_as_float(qa.x << 16); ya.y += __uint_as_float(qa.x & 0xFFFF0000u);
-                            ya.z += __uint_as_float(qa.y << 16); ya.w += __uint_as_float(qa.y & 0xFFFF0000u);
-                            yb.x += __uint_as_float(qb.x << 16); yb.y += __uint_as_float(qb.x & 0xFFFF0000u);
-                            yb.z += __uint_as_float(qb.y << 16); yb.w += __uint_as_float(qb.y & 0xFFFF0000u);
-                        } else {
-                            const uint32_t col = ((blk * 4 + t) ^ ((g & 1) * FY)) << 4;
-                            const uint4 qa = lds128(row_at + col), qb = lds128(row_at + 8 * CH * E + col);
-                            ya.x += __uint_as_float(qa.x); ya.y += __uint_as_float(qa.y);
-                            ya.z += __uint_as_float(qa.z); ya.w += __uint_as_float(qa.w);
-                            yb.x += __uint_as_float(qb.x); yb.y += __uint_as_float(qb.y);
-                            yb.z += __uint_as_float(qb.z); yb.w += __uint_as_float(qb.w);
-                        }
-                    }
-                    if constexpr (Y16) {
-                        auto pack = [](float4 v) {
-                            uint2 o;
-                            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o.x) : "f"(v.y), "f"(v.x));
-                            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o.y) : "f"(v.w), "f"(v.z));
-                            return o;
-                        };
-                        if (la) *reinterpret_cast<uint2 *>(ya_at + blk * 32) = pack(ya);
-                        if (lb) *reinterpret_cast<uint2 *>(yb_at + blk * 32) = pack(yb);
-                    } else {
-                        if (la) *reinterpret_cast<float4 *>(ya_at + blk * 64) = ya;
-                        if (lb) *reinterpret_cast<float4 *>(yb_at + blk * 64) = yb;
+                    for (int k = 0; k < RK / 32; ++k) {
+#pragma unroll
+                        for (int i = 0; i < TERMS; ++i)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) lora_mma(part[i][j], ha[i][2 * k], w[j][k].x, w[j][k].y);
+#pragma unroll
+                        for (int i = 0; i < TERMS; ++i)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) lora_mma(part[i][j], ha[i][2 * k + 1], w[j][k].z, w[j][k].w);
                     }
                 }
+                float d[2][4];
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        d[j][c] = part[TERMS - 1][j][c];
+#pragma unroll
+                        for (int i = TERMS - 2; i >= 0; --i) d[j][c] += part[i][j][c];
+                    }
+                float4 ya = make_float4(d[0][0], d[0][1], d[1][0], d[1][1]), yb = make_float4(d[0][2], d[0][3], d[1][2], d[1][3]);
+                const uint32_t row_at = st + kBase + ra * (CH * E);
+                if constexpr (Y16) {
+                    const uint2 none = make_uint2(0u, 0u);
+                    const uint2 qa = base ? lds64(row_at + blk * 32 + t * 8) : none, qb = base ? lds64(row_at + 8 * CH * E + blk * 32 + t * 8) : none;
+                    ya.x += __uint_as_float(qa.x << 16); ya.y += __uint_as_float(qa.x & 0xFFFF0000u);
+                    ya.z += __uint_as_float(qa.y << 16); ya.w += __uint_as_float(qa.y & 0xFFFF0000u);
+                    yb.x += __uint_as_float(qb.x << 16); yb.y += __uint_as_float(qb.x & 0xFFFF0000u);
+                    yb.z += __uint_as_float(qb.y << 16); yb.w += __uint_as_float(qb.y & 0xFFFF0000u);
+                    auto pack = [](float4 v) {
+                        uint2 o;
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o.x) : "f"(v.y), "f"(v.x));
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o.y) : "f"(v.w), "f"(v.z));
+                        return o;
+                    };
+                    if (la) *reinterpret_cast<uint2 *>(ya_at + blk * 32) = pack(ya);
+                    if (lb) *reinterpret_cast<uint2 *>(yb_at + blk * 32) = pack(yb);
+                } else {
+                    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+                    const uint32_t col = ((blk * 4 + t) ^ ((g & 1) * FY)) << 4;
+                    const uint4 qa = base ? lds128(row_at + col) : none, qb = base ? lds128(row_at + 8 * CH * E + col) : none;
+                    ya.x += __uint_as_float(qa.x); ya.y += __uint_as_float(qa.y);
+                    ya.z += __uint_as_float(qa.z); ya.w += __uint_as_float(qa.w);
+                    yb.x += __uint_as_float(qb.x); yb.y += __uint_as_float(qb.y);
+                    yb.z += __uint_as_float(qb.z); yb.w += __uint_as_float(qb.w);
+                    if (la) *reinterpret_cast<float4 *>(ya_at + blk * 64) = ya;
+                    if (lb) *reinterpret_cast<float4 *>(yb_at + blk * 64) = yb;
+                }
+            };
+            int left = n_ch;                                          // channels from this stage on
+#pragma unroll 1
+            for (int q = 0; q < n2; ++q, left -= CH) {
+                const uint32_t st = arrive(issue2);
+                // a whole stage without a condition between its blocks: the products of one fill the waits of another
+                auto all = [&](auto &&work) {
+                    if (left >= CH) {
+#pragma unroll
+                        for (int b0 = 0; b0 < CH / 16; b0 += WN) work(st, b0 + wr);
+                    } else {
+#pragma unroll 1
+                        for (int b0 = wr; b0 * 16 < left; b0 += WN) work(st, b0);
+                    }
+                };
+                if (live) all(block);
+                ya_at += CH * E; yb_at += CH * E;
             }
         }
         turn = (int)(((long long)turn + items) % clusters);
