@@ -332,24 +332,20 @@ w2a8_lora_kernel(const LoraParams p) {
                 src_y[i] = base + ((size_t)(chunk + sm.perm[at + row]) * N + ch0) * E + cy * 16;
             }
             const char *src_a = reinterpret_cast<const char *>(p.A[mat] + ((size_t)a * p.rank_max + rx) * p.K + u0 * 64 + cx * 8);
-            // Ranks of B behind the adapter's last, up to the end of a step of 32 (16), count as zero, whatever the row holds:
-            // of a piece, b_bytes are the adapter's.
+            // Ranks of B behind the adapter's last count as zero, whatever the row holds: of a piece, b_bytes are the adapter's
             const int b_bytes = min(max(r - cb * 8, 0), 8) * 2;
-            const bool b_zero = b_bytes == 0, b_piece = cb * 8 < (RK == 16 ? 16 : (r + 31) / 32 * 32);
-            const char *src_b = reinterpret_cast<const char *>(p.B[mat] + ((size_t)a * N + ch0 + rbb) * p.rank_max + (b_zero ? 0 : cb * 8));
+            const char *src_b = reinterpret_cast<const char *>(p.B[mat] + ((size_t)a * N + ch0 + rbb) * p.rank_max + (b_bytes ? cb * 8 : 0));
             const int b_step = DB * p.rank_max * 2, a_step = DX * p.K * 2;
             int q_issue = 0, slot_issue = 0;
             auto issue2 = [&]() {                                     // a stage of step 2
                 const uint32_t st = ring + slot_issue * STAGE;
                 const int cw = n_ch - (q_issue - n1) * CH;            // channels that are left
                 if (cw > 0) {
-                    if (b_piece) {
-                        const char *src = src_b;
+                    const char *src = src_b;
 #pragma unroll
-                        for (int i = 0; i < PB; ++i, src += b_step)
-                            if (rbb + i * DB < cw && (CH % DB == 0 || rbb + i * DB < CH))
-                                lora_copy_some(st + to_b + i * (kLoraThreads * 16), src, b_bytes);
-                    }
+                    for (int i = 0; i < PB; ++i, src += b_step)
+                        if (rbb + i * DB < cw && (CH % DB == 0 || rbb + i * DB < CH))
+                            lora_copy_some(st + to_b + i * (kLoraThreads * 16), src, b_bytes);
                     src_b += (size_t)CH * p.rank_max * 2;
                     if (base && cy * (16 / E) < cw) {
 #pragma unroll

@@ -65,3 +65,22 @@ def test_replayed_with_other_owners(gpu):                            # noqa: F81
         graph.replay()
         torch.cuda.synchronize()
         _equal(torch, y, _reference(torch, p["x"], p["adapter"], p["A"], p["B"], p["rank"], p["scale"], p["base"]))
+
+
+@pytest.mark.parametrize("rank_max", [16, 32, 64, 128])
+@pytest.mark.parametrize("tile", [16, 64])
+def test_low_ranks_beside_bits_of_nan(gpu, monkeypatch, tile, rank_max):   # noqa: F811
+    """Ranks far below what the storage is laid out for, while what else passes through the kernel's stages holds the bit
+    patterns of bf16 NaNs: the fp32 base values have them in their lower halves.  Nothing of it may meet the products."""
+    torch, b = gpu
+    monkeypatch.setenv("W2A8_LORA_TILE", str(tile))
+    M, Ns, K, L = 150, (1040, 272), 576, 5
+    p = _integers(torch, M, Ns, K, L, rank_max, seed=rank_max, ranks=[1, 3, 8, rank_max // 2 + 1, rank_max - 3])
+    for t in p["base"]:
+        bits = t.view(torch.int32)
+        bits.copy_((bits & -65536) | 0x7FC0)
+        assert bool(t.isfinite().all())
+    lora = b.LoraGroup(p["A"], p["B"], rank=p["rank"], scale=p["scale"])
+    for _ in range(2):
+        y = b.w2a8_lora_grouped(p["x"], p["adapter"], lora, base=p["base"])
+        _equal(torch, y, _reference(torch, p["x"], p["adapter"], p["A"], p["B"], p["rank"], p["scale"], p["base"]))
