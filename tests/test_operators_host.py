@@ -43,7 +43,7 @@ def test_lora_refusals(lib, mem):
     assert call(count=0) == SHAPE and call(count=5) == SHAPE
     assert call(adapters=0) == SHAPE and call(adapters=1025) == SHAPE
     assert call(rank_max=0) == SHAPE and call(rank_max=12) == SHAPE and call(rank_max=136) == SHAPE
-    assert call(M=0) == SHAPE and call(M=-1) == SHAPE and call(K=96) == SHAPE and call(K=0) == SHAPE
+    assert call(M=0) == SHAPE and call(M=-1) == SHAPE and call(M=(1 << 30) + 1) == SHAPE and call(K=96) == SHAPE and call(K=0) == SHAPE
     assert call(n=(ctypes.c_int * 1)(24)) == SHAPE and call(n=(ctypes.c_int * 1)(0)) == SHAPE
     assert call(x=x + 8) == ALIGN and call(ad=ad + 2) == ALIGN and call(rank=ad + 1) == ALIGN and call(scale=ad + 2) == ALIGN
     assert call(A=_ptrs(p + 8)) == ALIGN and call(B=_ptrs(p + 8)) == ALIGN
