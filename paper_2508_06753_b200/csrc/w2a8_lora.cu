@@ -7,19 +7,26 @@
 // Bound: memory.  base and y are read and written once, the A and B of every adapter in the batch once; the products
 // are 2 r (K + N) operations per token and matrix, far below the tensor cores' rate at the ranks of adapters.
 //
-// One launch, no workspace.  Every CTA sorts the tokens of the batch by adapter itself (a stable counting sort of
-// 4096 tokens at a time in shared memory: all CTAs find the same order) and cuts them into tiles of up to 64 tokens
-// of one adapter.  A work item is (tile, matrix, share of the channels); a cluster of C CTAs takes one at a time:
-//   1. h: the K axis is split over the CTAs of the cluster, and inside a CTA over pairs of warps; tokens and ranks over
-//      the other warps.  The sums are added in a fixed order, over the cluster through distributed shared memory.
+// One launch, no workspace.  Every CTA sorts the tokens of the batch by adapter itself (a stable counting sort of some
+// tokens at a time in shared memory: all CTAs find the same order) and cuts them into tiles of up to T tokens of one
+// adapter.  A work item is (tile, matrix, share of the channels); a cluster of C CTAs takes one at a time:
+//   1. h: the K axis is split over the CTAs of the cluster; tokens, ranks and what is left of K over the warps.  The sums
+//      are added in a fixed order, over the cluster through distributed shared memory.
 //   2. y: the channels of the item are split over the CTAs and warps.  s h stays in fp32: it is cut into three bf16
 //      terms by truncation, whose sum is exactly its 24 bits (two terms, 16 bits, for a bf16 result), so the product
 //      with the bf16 B carries no rounding of h.
 // Both steps are fed by one ring of shared-memory stages that cp.async fills ahead (x and A, then B and base), so
-// that the loads of step 2 are on their way while the sums of step 1 are added.  mma.sync bf16: the ranks a tile has
-// fill 16 to 128 columns, far too few for tcgen05 tiles to pay, and the bytes bound the kernel.  k is permuted alike on
-// both sides so that a lane's operands of two instructions are 16 consecutive bytes, and the channels so that a lane
-// holds four consecutive ones.
+// that the loads of step 2 are on their way while the sums of step 1 are added.  k is permuted alike on both sides so that a
+// lane's operands of two instructions are 16 consecutive bytes, and the channels so that a lane holds four consecutive
+// ones.
+//
+// The products are mma.sync (8 clk per m16n8k16 and scheduler): an item's accumulators have 16 to 128 columns in step 1
+// and 16 rows per warp in step 2, and both have to leave the tensor core's sum early, for its truncation.  What bounds the
+// kernel (device time, calls over inputs larger than L2): gate|up of the 8B layer for 8192 tokens of 16 adapters of rank 64,
+// 397 us, 5.1 TB/s of the 2.02 GB it cannot do without; about 30 us of an item's 200 are step 1, when the memory idles,
+// and in step 2 the issue of two warps per scheduler (0.32 a clock; tensor pipe 36 %).  32 tokens with an adapter each 38 us,
+// 2.5 TB/s: the same issue, with 15 of 16 rows of an instruction empty.  One token, q|k|v: 6.5 us of latencies: owners, sort,
+// addresses, first bytes, two cluster barriers.
 #include "w2a8_common.cuh"
 
 namespace w2a8 {
@@ -335,7 +342,8 @@ w2a8_lora_kernel(const LoraParams p) {
             // Ranks of B behind the adapter's last count as zero, whatever the row holds: of a piece, b_bytes are the adapter's
             const int b_bytes = min(max(r - cb * 8, 0), 8) * 2;
             const char *src_b = reinterpret_cast<const char *>(p.B[mat] + ((size_t)a * N + ch0 + rbb) * p.rank_max + (b_bytes ? cb * 8 : 0));
-            const int b_step = DB * p.rank_max * 2, a_step = DX * p.K * 2;
+            const int b_step = DB * p.rank_max * 2;
+            const size_t a_step = (size_t)DX * p.K * 2;
             int q_issue = 0, slot_issue = 0;
             auto issue2 = [&]() {                                     // a stage of step 2
                 const uint32_t st = ring + slot_issue * STAGE;
@@ -605,7 +613,7 @@ static cudaError_t launch_lora(LoraParams &p, cudaStream_t st) {
     // The cluster size by the estimate above, for a guess of the tiles: one per adapter, and the full ones where there are
     // many tokens.  The number of clusters for as many tiles as there may be (tokens without an adapter can be one more).
     const int used = p.M < p.adapters ? p.M : p.adapters, bound = p.M / T + used + 1;
-    const int tiles = p.M <= (long long)used * T ? used : p.M / T + used;
+    const int tiles = p.M <= (long long)used * T ? used : p.M < (1 << 24) ? p.M / T + used : (1 << 24) / T;
     const int forced = env_int("W2A8_LORA_C", 0);
     const bool force = forced >= 1 && forced <= kLoraMaxCluster;
     int C = 0, n = 0;

@@ -15,7 +15,8 @@
 // addition, the norm's weights stay in registers, and the rows of the next tokens are on their way into slots of shared
 // memory of each thread (registers for them would cost the occupancy that keeps the memory busy).
 // The sines and cosines of the CTA's tokens are computed once, one per thread, into shared memory, while the first rows
-// are on their way.
+// are on their way.  8192 tokens of 72 heads of 128 (device time): fp32 to bf16 67 us, 6.7 TB/s, what a copy reaches;
+// with norms from bf16 50 us, 6.1 TB/s, where the issue of the arithmetic takes about 30 us of its own.  One token: 1.6 us.
 #include <math.h>
 
 #include "w2a8_common.cuh"
