@@ -316,10 +316,22 @@ w2a8_lora_kernel(const LoraParams p) {
 
             if (r == 0) {                                             // nothing to add
                 if (base == y) continue;
+                // a warp takes a row; eight 16-byte pieces of a lane are on their way at a time
+                constexpr int kAhead = 8;
                 const int row_v = n_ch * E / 16;
-                for (int i = tid; i < n * row_v; i += kLoraThreads) {
-                    const size_t off = ((size_t)(chunk + sm.perm[at + i / row_v]) * N + ch0) * E + (size_t)(i % row_v) * 16;
-                    *reinterpret_cast<uint4 *>(y + off) = base ? *reinterpret_cast<const uint4 *>(base + off) : make_uint4(0u, 0u, 0u, 0u);
+                for (int row = warp; row < n; row += kLoraWarps) {
+                    const size_t off = ((size_t)(chunk + sm.perm[at + row]) * N + ch0) * E;
+                    const uint4 *from = reinterpret_cast<const uint4 *>(base + off);
+                    uint4 *to = reinterpret_cast<uint4 *>(y + off);
+                    for (int c = lane; c < row_v; c += 32 * kAhead) {
+                        uint4 v[kAhead];
+#pragma unroll
+                        for (int i = 0; i < kAhead; ++i)
+                            v[i] = base && c + 32 * i < row_v ? from[c + 32 * i] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                        for (int i = 0; i < kAhead; ++i)
+                            if (c + 32 * i < row_v) to[c + 32 * i] = v[i];
+                    }
                 }
                 continue;
             }
@@ -610,10 +622,14 @@ static cudaError_t launch_lora(LoraParams &p, cudaStream_t st) {
             n[C] = found > 0 ? found : sm_count() / C;
         }
     });
-    // The cluster size by the estimate above, for a guess of the tiles: one per adapter, and the full ones where there are
-    // many tokens.  The number of clusters for as many tiles as there may be (tokens without an adapter can be one more).
-    const int used = p.M < p.adapters ? p.M : p.adapters, bound = p.M / T + used + 1;
-    const int tiles = p.M <= (long long)used * T ? used : p.M < (1 << 24) ? p.M / T + used : (1 << 24) / T;
+    // The cluster size by the estimate above, for a guess of the tiles.  Decode batches: one per adapter that there is a token
+    // for.  Many tokens: the full ones and one more per adapter, but no more of these than of the full ones and two (resident
+    // adapters need not be in use: 600 tokens of 6 of 60 adapters of rank 16, 4096 x 4096, take 18.8 us with the clusters of
+    // two that 60 tiles ask for, 15.8 with the four of this guess).  The number of clusters is for as many tiles as there may
+    // be (tokens without an adapter can be one more).
+    const int used = p.M < p.adapters ? p.M : p.adapters, full = p.M / T, bound = full + used + 1;
+    const int more = used < full + 2 ? used : full + 2;
+    const int tiles = T == 16 && p.M <= (long long)used * T ? used : p.M < (1 << 24) ? full + more : (1 << 24) / T;
     const int forced = env_int("W2A8_LORA_C", 0);
     const bool force = forced >= 1 && forced <= kLoraMaxCluster;
     int C = 0, n = 0;
@@ -640,9 +656,11 @@ static cudaError_t launch_lora(LoraParams &p, cudaStream_t st) {
 
 template <int RK>
 static cudaError_t launch_lora_rank(LoraParams &p, bool y16, cudaStream_t st) {
-    // Tiles of 16 tokens for decode batches: few tokens, or many adapters for the tokens (at 256 tokens of 64 adapters of
-    // rank 64 tiles of 64 take 209 us, of 16 76; with one adapter 29 and 26; at 1024 tokens of 4 adapters 56 and 73).
-    const int tile = env_int("W2A8_LORA_TILE", p.M <= 256 || p.M <= 4 * p.adapters ? 16 : 64);
+    // Tiles of 16 tokens for decode batches: few tokens, or many adapters for the tokens.  Tiles of 16 / 64, us: 256 tokens of
+    // 64 adapters of rank 64, gate|up of the 8B layer, 68 / 209, 300 tokens 90 / 185; 256 tokens of one adapter 27 / 29; 1024
+    // tokens of 4 adapters of rank 32 73 / 62; 500 tokens, q|k|v, rank 32, 64 resident adapters: 64 in use 36 / 72, 5 in use
+    // 31 / 22.
+    const int tile = env_int("W2A8_LORA_TILE", p.M <= 256 || p.M <= 8 * p.adapters ? 16 : 64);
     if (tile == 16) return y16 ? launch_lora<16, RK, true>(p, st) : launch_lora<16, RK, false>(p, st);
     return y16 ? launch_lora<64, RK, true>(p, st) : launch_lora<64, RK, false>(p, st);
 }
