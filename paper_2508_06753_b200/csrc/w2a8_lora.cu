@@ -23,7 +23,7 @@
 // The products are mma.sync (8 clk per m16n8k16 and scheduler): an item's accumulators have 16 to 128 columns in step 1
 // and 16 rows per warp in step 2, and both have to leave the tensor core's sum early, for its truncation.  What bounds the
 // kernel (device time, calls over inputs larger than L2): gate|up of the 8B layer for 8192 tokens of 16 adapters of rank 64,
-// 397 us, 5.1 TB/s of the 2.02 GB it cannot do without; about 30 us of an item's 200 are step 1, when the memory idles,
+// 400 us, 5.0 TB/s of the 2.02 GB it cannot do without; about 30 us of an item's 200 are step 1, when the memory idles,
 // and in step 2 the issue of two warps per scheduler (0.32 a clock; tensor pipe 36 %).  32 tokens with an adapter each 38 us,
 // 2.5 TB/s: the same issue, with 15 of 16 rows of an instruction empty.  One token, q|k|v: 6.5 us of latencies: owners, sort,
 // addresses, first bytes, two cluster barriers.
@@ -491,6 +491,7 @@ w2a8_lora_kernel(const LoraParams p) {
                     *reinterpret_cast<float4 *>(&sm.h[off]) = v;
                 }
             }
+            __syncwarp();                                             // the cluster barrier is for whole warps
             if (C > 1) { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); reading = true; }
             __syncthreads();
 
@@ -605,6 +606,7 @@ w2a8_lora_kernel(const LoraParams p) {
         turn = (int)(((long long)turn + items) % clusters);
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncwarp();
     if (reading) cluster_wait();                                      // nobody leaves while its sums may be read
 }
 
