@@ -402,8 +402,10 @@ int w2a8_linear_grouped_host(const void *x_host, int M, int K, int count, const 
  *   y[i][m][n] = base[i][m][n] + sum_{j < r} B[i][a][n][j] * (s * h[j])
  * A token whose adapter[m] lies outside [0, adapters) has none: y = base, bit
  * for bit.  Sums are held in fp32, s * h is not rounded below 24 bits for an
- * fp32 result (16 bits for a bf16 one), and y is rounded once.  Values of A and
- * B at ranks of r and more are not used, whatever they hold.
+ * fp32 result (cut to 16 bits for a bf16 one, by less than 2^-15 of it), and y is
+ * rounded once.  Infinities and NaN among x, A, B and base follow the formula and
+ * stay in their tokens and channels.  Values of A and B at ranks of r and more are
+ * not used, whatever they hold.
  *   x_bf16   [M][K] bf16, row-major
  *   adapter  [M] int32, in any order (4-byte alignment suffices)
  *   rank     [adapters] int32, clamped to 0 .. rank_max, or NULL: rank_max for all
