@@ -59,6 +59,19 @@ __device__ __forceinline__ float4 lora_ld_cluster(uint32_t local, uint32_t rank)
                  : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote) : "memory");
     return v;
 }
+// The cluster's barriers are for whole warps, and the code in front of them branches by lane.
+__device__ __forceinline__ void lora_cluster_sync() {
+    __syncwarp();
+    cluster_sync();
+}
+__device__ __forceinline__ void lora_cluster_arrive() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void lora_cluster_wait() {
+    __syncwarp();
+    cluster_wait();
+}
 __device__ __forceinline__ void lora_copy16(uint32_t to, const void *from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
@@ -447,7 +460,7 @@ w2a8_lora_kernel(const LoraParams p) {
                         for (int c = 0; c < 4; ++c) acc[j][c] += d[j][c];
                 }
             }
-            if (reading) { cluster_wait(); reading = false; }         // the shares of the item before have been read
+            if (reading) { lora_cluster_wait(); reading = false; }    // the shares of the item before have been read
 #pragma unroll
             for (int k = NK - 1; k >= 0; --k) {
                 if (jk == k && live) {
@@ -464,7 +477,7 @@ w2a8_lora_kernel(const LoraParams p) {
                 }
                 if (k > 0) __syncthreads();
             }
-            if (C > 1) cluster_sync(); else __syncthreads();
+            if (C > 1) lora_cluster_sync(); else __syncthreads();
             {
                 // columns of ranks that the adapter has not (sums with whatever the stage held) count as zero
                 constexpr int C4 = RK / 4;
@@ -492,8 +505,7 @@ w2a8_lora_kernel(const LoraParams p) {
                     *reinterpret_cast<float4 *>(&sm.h[off]) = v;
                 }
             }
-            __syncwarp();                                             // the cluster barrier is for whole warps
-            if (C > 1) { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); reading = true; }
+            if (C > 1) { lora_cluster_arrive(); reading = true; }
             __syncthreads();
 
             // ---- step 2 -------------------------------------------------------------------------------------------
@@ -652,8 +664,7 @@ w2a8_lora_kernel(const LoraParams p) {
         turn = (int)(((long long)turn + items) % clusters);
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
-    __syncwarp();
-    if (reading) cluster_wait();                                      // nobody leaves while its sums may be read
+    if (reading) lora_cluster_wait();                                 // nobody leaves while its sums may be read
 }
 
 template <int T, int RK, bool Y16>
