@@ -415,7 +415,7 @@ int w2a8_linear_grouped_host(const void *x_host, int M, int K, int count, const 
  *   base, y  HOST arrays of `count` DEVICE pointers to [M][N[i]], fp32 or (both)
  *            bf16.  base[i] == y[i] adds in place (the rows of tokens without an
  *            adapter are then left alone); base == NULL counts as zero.
- *            Otherwise y[i] overlaps neither x, base nor another y
+ *            Otherwise y[i] overlaps nothing that the call reads and no other y
  *            (W2A8_ERR_SHAPE).
  *   N        HOST array of `count` entries
  * 1 <= adapters <= 1024, rank_max a multiple of 8 up to 128, M (up to 2^30), N

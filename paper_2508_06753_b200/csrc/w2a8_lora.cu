@@ -753,16 +753,20 @@ extern "C" int w2a8_lora_grouped(const void *x_bf16, const int32_t *adapter, int
         p.y[i] = y[i];
         p.N[i] = N[i];
     }
-    // a result may take the place of its own base and overlaps nothing else that the call reads or writes
+    // A result may take the place of its own base and overlaps nothing else that the call reads or writes: CTAs read all of
+    // it while others write.
     auto overlap = [](const void *q, size_t nq, const void *r, size_t nr) {
         const char *a = static_cast<const char *>(q), *b = static_cast<const char *>(r);
         return r && a < b + nr && b < a + nq;
     };
     for (int i = 0; i < count; ++i) {
         const size_t ny = (size_t)M * N[i] * e;
-        if (overlap(y[i], ny, x_bf16, (size_t)M * K * 2)) return W2A8_ERR_SHAPE;
+        if (overlap(y[i], ny, x_bf16, (size_t)M * K * 2) || overlap(y[i], ny, adapter, (size_t)M * 4) ||
+            overlap(y[i], ny, rank, (size_t)adapters * 4) || overlap(y[i], ny, scale, (size_t)adapters * 4))
+            return W2A8_ERR_SHAPE;
         for (int j = 0; j < count; ++j) {
-            const size_t nj = (size_t)M * N[j] * e;
+            const size_t nj = (size_t)M * N[j] * e, one = (size_t)adapters * rank_max * 2;
+            if (overlap(y[i], ny, A[j], one * K) || overlap(y[i], ny, B[j], one * N[j])) return W2A8_ERR_SHAPE;
             if (j != i && overlap(y[i], ny, y[j], nj)) return W2A8_ERR_SHAPE;
             if (overlap(y[i], ny, p.base[j], nj) && !(i == j && p.base[j] == y[i])) return W2A8_ERR_SHAPE;
         }
