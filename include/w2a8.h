@@ -475,7 +475,8 @@ int w2a8_rope_frequencies(int rot_dim, double base, int scaling, double factor, 
  *                (W2A8_ERR_SHAPE).  Column ranges of the same wider rows do not
  *                overlap.  Elements between the rows are neither read nor written.
  *   positions    [M] int32;  inv_freq  [rot_dim / 2] double (8-byte alignment)
- * head_dim even, 2 .. 512; rot_dim even, 2 .. head_dim.  Head sizes, rot_dim and
+ * M up to 2^30; head_dim even, 2 .. 512; rot_dim even, 2 .. head_dim; at most
+ * 2^17 heads in all.  Head sizes, rot_dim and
  * strides that are multiples of 8 take 16-byte accesses.
  */
 int w2a8_rope(int count, const void *const *x, int x_is_bf16, void *const *out, int out_is_bf16, const int *heads,

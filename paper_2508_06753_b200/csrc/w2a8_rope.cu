@@ -304,7 +304,9 @@ static cudaError_t launch_rope(RopeParams &p, int vec, bool x16, bool o16, cudaS
     while (p.tokens_per_block < 8 && 2 * p.tokens_per_block * p.half <= kRopeTurns &&
            (long long)p.M / (2 * p.tokens_per_block) * gy * threads >= 1150ll * sm_count())
         p.tokens_per_block *= 2;
-    const dim3 grid((unsigned)((p.M + p.tokens_per_block - 1) / p.tokens_per_block) * gy);
+    const long long ctas = (long long)((p.M + p.tokens_per_block - 1) / p.tokens_per_block) * gy;
+    if (ctas > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;        // rows that no memory holds
+    const dim3 grid((unsigned)ctas);
     if (V == 1) return launch_rope_layout<1, 8, NORM>(p, x16, o16, grid, threads, st);
     if (V == 8) return launch_rope_layout<8, 1, NORM>(p, x16, o16, grid, threads, st);
     return units <= 32 ? launch_rope_layout<4, 1, NORM>(p, x16, o16, grid, threads, st)
@@ -341,7 +343,8 @@ static int rope_common(bool norm, int count, const void *const *x, int x_is_bf16
                        const int64_t *out_strides, int M, int head_dim, int rot_dim, int interleaved,
                        const int32_t *positions, const double *inv_freq, float amplitude, void *stream) {
     if (!x || !out || !heads || !x_strides || !out_strides) return W2A8_ERR_NULL;
-    if (count < 1 || count > kRopeMaxTensors || M < 1 || head_dim < 2 || head_dim > kRopeMaxDim || head_dim % 2 ||
+    // tokens are counted in 32 bits, a CTA's share ahead
+    if (count < 1 || count > kRopeMaxTensors || M < 1 || M > (1 << 30) || head_dim < 2 || head_dim > kRopeMaxDim || head_dim % 2 ||
         rot_dim < (norm ? 0 : 2) || rot_dim > head_dim || rot_dim % 2)
         return W2A8_ERR_SHAPE;
     if (norm && !(eps >= 0.0f)) return W2A8_ERR_SHAPE;
@@ -372,7 +375,7 @@ static int rope_common(bool norm, int count, const void *const *x, int x_is_bf16
         p.t[i] = {x[i], out[i], norm && weight ? weight[i] : nullptr, xt, xh, ot, oh};
         rows += H;
         p.end[i] = rows;
-        if (rows > (1 << 17)) return W2A8_ERR_SHAPE;             // the grid's limit, at two rows per CTA and more
+        if (rows > (1 << 17)) return W2A8_ERR_SHAPE;             // rows times lanes of a row stay small numbers of 32 bits
     }
     for (int i = 0; i < count; ++i)
         for (int j = 0; j < count; ++j) {
