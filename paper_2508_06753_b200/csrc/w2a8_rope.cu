@@ -359,10 +359,11 @@ static int rope_common(bool norm, int count, const void *const *x, int x_is_bf16
         const long long xt = x_strides[2 * i], xh = x_strides[2 * i + 1];
         const long long ot = out_strides[2 * i], oh = out_strides[2 * i + 1];
         const int H = heads[i];
-        constexpr long long kMax = 1ll << 40;
-        if (H < 1 || H > (1 << 17) || xt < 0 || xh < 0 || ot < 0 || oh < 0 || xt > kMax || xh > kMax || ot > kMax ||
-            oh > kMax)
-            return W2A8_ERR_SHAPE;
+        if (H < 1 || H > (1 << 17)) return W2A8_ERR_SHAPE;
+        // from the first row to the last: more than any memory, and far from the end of 64 bits in what follows
+        constexpr long long kMax = 1ll << 48;
+        auto fits = [](long long stride, int n) { return stride >= 0 && stride <= kMax / (n > 1 ? n - 1 : 1); };
+        if (!fits(xt, M) || !fits(xh, H) || !fits(ot, M) || !fits(oh, H)) return W2A8_ERR_SHAPE;
         // rows of the result must not share elements: heads inside tokens, or tokens inside heads
         const bool by_token = (H == 1 || oh >= head_dim) && (M == 1 || ot >= (long long)(H - 1) * oh + head_dim);
         const bool by_head = (M == 1 || ot >= head_dim) && (H == 1 || oh >= (long long)(M - 1) * ot + head_dim);

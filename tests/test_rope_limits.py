@@ -38,3 +38,19 @@ def test_tokens(lib, mem, M, norm):
     _, p = mem
     far = p + (1 << 40)
     assert _call(lib, norm, [p], [far], p, p, M, [1], 2, 2, [(2, 2)], [(2, 2)], x16=1, o16=1) == SHAPE
+
+
+@pytest.mark.parametrize("norm", [False, True])
+def test_strides(lib, mem, norm):
+    """Rows whose last lies 2^64 bytes and more behind the first, where sums of 64 bits come round: two results over each
+    other, a result over its input, an input and a result alone."""
+    _, p = mem
+    D, far = 64, p + 65536
+    call = lambda *a: _call(lib, norm, *a[:2], p, p, *a[2:])
+    M, wide, sane = 1 << 30, (1 << 40, D), (2 * D, D)
+    assert call([p, p + (1 << 41)], [far, far], M, [2, 2], D, D, [sane] * 2, [wide] * 2) == SHAPE
+    assert call([p], [p], M, [2], D, D, [sane], [wide]) == SHAPE
+    assert call([p], [far], M, [2], D, D, [wide], [wide]) == SHAPE
+    assert call([p], [far], M, [2], D, D, [wide], [sane]) == SHAPE
+    heads = 1 << 17                                                     # the same by heads
+    assert call([p], [p], 2, [heads], D, D, [(D, 2 * D)], [(D, 1 << 47)]) == SHAPE
