@@ -471,8 +471,8 @@ int w2a8_rope_frequencies(int rot_dim, double base, int scaling, double factor, 
  *   x_strides, out_strides   HOST, [count][2]: elements between tokens and
  *                between heads; the values of a head are consecutive.  Rows of
  *                `out` may not share elements; out[i] may be x[i] (same type and
- *                strides), and otherwise no out overlaps an x or another out
- *                (W2A8_ERR_SHAPE).  Column ranges of the same wider rows do not
+ *                strides), and otherwise no out overlaps an x, another out or
+ *                anything else that the call reads (W2A8_ERR_SHAPE).  Column ranges of the same wider rows do not
  *                overlap.  Elements between the rows are neither read nor written.
  *   positions    [M] int32;  inv_freq  [rot_dim / 2] double (8-byte alignment)
  * M up to 2^30; head_dim even, 2 .. 512; rot_dim even, 2 .. head_dim; at most

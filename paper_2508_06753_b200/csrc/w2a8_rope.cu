@@ -338,6 +338,11 @@ static bool rows_meet(const RowSet &a, const RowSet &b) {
     return true;
 }
 
+// Whether a set may share bytes with a plain array, which stands as one row of the set's strides.
+static bool rows_meet_array(const RowSet &a, const void *array, long long bytes) {
+    return array && rows_meet(a, {static_cast<const char *>(array), a.token, a.head, 1, 1, bytes});
+}
+
 static int rope_common(bool norm, int count, const void *const *x, int x_is_bf16, void *const *out, int out_is_bf16,
                        const float *const *weight, float eps, const int *heads, const int64_t *x_strides,
                        const int64_t *out_strides, int M, int head_dim, int rot_dim, int interleaved,
@@ -385,7 +390,11 @@ static int rope_common(bool norm, int count, const void *const *x, int x_is_bf16
             const bool same = i == j && in[i].at == to[i].at && xe == oe && (M == 1 || in[i].token == to[i].token) &&
                               (heads[i] == 1 || in[i].head == to[i].head);
             if (!same && rows_meet(to[i], in[j])) return W2A8_ERR_SHAPE;
+            // CTAs read these while others write
+            if (rows_meet_array(to[i], p.t[j].weight, head_dim * 4ll)) return W2A8_ERR_SHAPE;
         }
+    for (int i = 0; rot_dim > 0 && i < count; ++i)
+        if (rows_meet_array(to[i], positions, M * 4ll) || rows_meet_array(to[i], inv_freq, rot_dim * 4ll)) return W2A8_ERR_SHAPE;
     if ((reinterpret_cast<uintptr_t>(positions) & 3u) || (reinterpret_cast<uintptr_t>(inv_freq) & 7u)) return W2A8_ERR_ALIGN;
     if (int st = check_device()) return st;
     p.rows = rows;

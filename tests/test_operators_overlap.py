@@ -42,3 +42,34 @@ def test_adapters_result_over_another_input(lib, mem):
         assert call((last, y1)) == SHAPE and call((y0, last)) == SHAPE
         for i, first in enumerate((at + 16 - M * Ns[0] * e, at + 16 - M * Ns[1] * e)):
             assert call((first, y1) if i == 0 else (y0, first)) == SHAPE
+
+
+@pytest.mark.parametrize("norm", [False, True])
+def test_rotated_result_over_another_input(lib, mem, norm):
+    """Positions, frequencies and weights; beside the rows of a wider result they are not refused for it."""
+    _, p = mem
+    M, H, D, wide = 5, 2, 64, 256                           # rows of 256 values, 128 of them the result's
+    x, pos, freq, w, out = (p + i * 65536 for i in range(5))
+
+    def call(out, pos=pos, freq=freq, w=w, rot=D):
+        s = lambda *v: (ctypes.c_int64 * 2)(*v)
+        mid = [_ptrs(w), 1e-6] if norm else []
+        return (lib.w2a8_qk_norm_rope if norm else lib.w2a8_rope)(
+            1, _ptrs(x), 0, _ptrs(out), 0, *mid, (ctypes.c_int * 1)(H), s(H * D, D), s(wide, D), M, D, rot, 0, pos, freq, 1.0, None)
+
+    free = call(out)                                        # whatever a call without a fault returns here
+    assert free != SHAPE
+    row = wide * 4
+    for name, at, n in [("pos", pos, M * 4), ("freq", freq, D // 2 * 8)] + ([("w", w, D * 4)] if norm else []):
+        assert call(at) == SHAPE
+        assert call(at + (n - 1) // 16 * 16) == SHAPE       # the first row begins in its last bytes
+        assert call(at + 16 - H * D * 4) == SHAPE           # the first row ends in its first
+        assert call(at - 3 * row - 64) == SHAPE             # inside the fourth row
+        kept = {name: out + 2 * row + H * D * 4}            # behind the third row, before the fourth
+        assert call(out, **kept) == free
+        kept = {name: out + 2 * row + H * D * 4 - 16}
+        assert call(out, **kept) == SHAPE
+        kept = {name: out + 3 * row - 16}
+        assert call(out, **kept) == (free if n <= 16 else SHAPE)
+    if norm:
+        assert call(out, pos=out, freq=out, rot=0) != SHAPE            # not read without a rotation
