@@ -466,7 +466,8 @@ int w2a8_rope_frequencies(int rot_dim, double base, int scaling, double factor, 
  * any size), the rest is fp32, rounded once.  Positions may be negative: the
  * rotation by -position undoes one, or moves rows that were rotated before.
  *   x, out       HOST arrays of `count` DEVICE pointers; fp32 or bf16 each
- *                (x_is_bf16, out_is_bf16), 16-byte aligned
+ *                (x_is_bf16, out_is_bf16); 16-byte aligned where head_dim,
+ *                rot_dim and all strides are multiples of 8, else as their type
  *   heads        HOST, [count]: heads of result i
  *   x_strides, out_strides   HOST, [count][2]: elements between tokens and
  *                between heads; the values of a head are consecutive.  Rows of

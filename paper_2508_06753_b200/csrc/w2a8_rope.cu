@@ -373,7 +373,6 @@ static int rope_common(bool norm, int count, const void *const *x, int x_is_bf16
         const bool by_token = (H == 1 || oh >= head_dim) && (M == 1 || ot >= (long long)(H - 1) * oh + head_dim);
         const bool by_head = (M == 1 || ot >= head_dim) && (H == 1 || oh >= (long long)(M - 1) * ot + head_dim);
         if (!by_token && !by_head) return W2A8_ERR_SHAPE;
-        if (!aligned16(x[i]) || !aligned16(out[i])) return W2A8_ERR_ALIGN;
         if (norm && weight && weight[i] && (reinterpret_cast<uintptr_t>(weight[i]) & 3u)) return W2A8_ERR_ALIGN;
         in[i] = {static_cast<const char *>(x[i]), xt * xe, xh * xe, M, H, (long long)head_dim * xe};
         to[i] = {static_cast<const char *>(out[i]), ot * oe, oh * oe, M, H, (long long)head_dim * oe};
@@ -395,6 +394,11 @@ static int rope_common(bool norm, int count, const void *const *x, int x_is_bf16
         }
     for (int i = 0; rot_dim > 0 && i < count; ++i)
         if (rows_meet_array(to[i], positions, M * 4ll) || rows_meet_array(to[i], inv_freq, rot_dim * 4ll)) return W2A8_ERR_SHAPE;
+    // pointers: to the accesses' size, 16 bytes or (single values) the type's
+    for (int i = 0; i < count; ++i)
+        if ((reinterpret_cast<uintptr_t>(x[i]) & (vec > 1 ? 15u : xe - 1u)) ||
+            (reinterpret_cast<uintptr_t>(out[i]) & (vec > 1 ? 15u : oe - 1u)))
+            return W2A8_ERR_ALIGN;
     if ((reinterpret_cast<uintptr_t>(positions) & 3u) || (reinterpret_cast<uintptr_t>(inv_freq) & 7u)) return W2A8_ERR_ALIGN;
     if (int st = check_device()) return st;
     p.rows = rows;

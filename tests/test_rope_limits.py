@@ -54,3 +54,21 @@ def test_strides(lib, mem, norm):
     assert call([p], [far], M, [2], D, D, [wide], [sane]) == SHAPE
     heads = 1 << 17                                                     # the same by heads
     assert call([p], [p], 2, [heads], D, D, [(D, 2 * D)], [(D, 1 << 47)]) == SHAPE
+
+
+@pytest.mark.parametrize("norm", [False, True])
+def test_alignment_of_single_values(lib, mem, norm):
+    """Heads, rotated parts or strides that are no multiple of 8 go value by value: as aligned as their type, so that a view
+    behind odd heads of the same rows is taken.  Of others every one has to be 16-byte aligned."""
+    _, p = mem
+    far, arrays = p + 65536, p + 131072
+    call = lambda x, out, D, rot, xs, os, **t: _call(lib, norm, [x], [out], arrays, arrays + 4096, 3, [2], D, rot, [xs], [os], **t)
+    for t, e in (dict(x16=1, o16=1), 2), (dict(x16=0, o16=0), 4):
+        fine = call(p, far, 30, 30, (150, 30), (60, 30), **t)       # whatever a call without a fault returns here
+        assert fine not in (SHAPE, ALIGN)
+        for D, rot, xs, os in [(30, 30, (150, 30), (60, 30)), (64, 36, (320, 64), (128, 64)), (64, 64, (324, 64), (128, 64)),
+                               (64, 64, (320, 64), (132, 66))]:
+            assert call(p + e, far, D, rot, xs, os, **t) == fine and call(p, far + e, D, rot, xs, os, **t) == fine
+            assert call(p + 1, far, D, rot, xs, os, **t) == ALIGN and call(p, far + e // 2, D, rot, xs, os, **t) == ALIGN
+        assert call(p + 8, far, 64, 64, (320, 64), (128, 64), **t) == ALIGN
+        assert call(p, far + 8, 64, 64, (320, 64), (128, 64), **t) == ALIGN
