@@ -395,6 +395,13 @@ def _want(t: torch.Tensor, name: str, dtype, shape, device):
         raise ValueError(f"{name} must be contiguous")
 
 
+def _c_ints(**sizes):
+    """Refuses sizes that the library's ints would not hold: ctypes hands on their lower 32 bits."""
+    for name, n in sizes.items():
+        if not -2 ** 31 <= n < 2 ** 31:
+            raise ValueError(f"{name} is {n}: more than 32 bits")
+
+
 def _launch_stream(device, index, stream) -> int:
     """Raw handle of the stream to launch on.  The launch goes to the current device: tensors of another one (`index`;
     -1: not on a GPU) are refused, and so is a stream of another."""
@@ -422,6 +429,7 @@ class LoraGroup:
             raise ValueError("A and B must be lists of one tensor per matrix")
         self.adapters, self.rank_max, self.K = (int(n) for n in self.A[0].shape)
         self.N = [int(b.shape[1]) for b in self.B]
+        _c_ints(adapters=self.adapters, rank_max=self.rank_max, K=self.K, N=max(self.N))
         self.device, self.index = self.A[0].device, self.A[0].get_device()
         for a, b, n in zip(self.A, self.B, self.N):
             _want(a, "A", torch.bfloat16, (self.adapters, self.rank_max, self.K), self.device)
@@ -484,6 +492,7 @@ def w2a8_rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "p
     w2a8_rope_frequencies in include/w2a8.h."""
     if scaling not in ROPE_SCALINGS:
         raise ValueError(f"scaling must be one of {sorted(ROPE_SCALINGS)}")
+    _c_ints(rot_dim=rot_dim, original_length=original_length)
     freq = torch.empty(max(int(rot_dim) // 2, 1), dtype=torch.float64)
     amplitude = ctypes.c_float()
     _check(lib().w2a8_rope_frequencies(rot_dim, base, ROPE_SCALINGS[scaling], factor, low, high, original_length,
@@ -503,6 +512,7 @@ class Heads:
         if not 1 <= self.count <= 4:
             raise ValueError("1 to 4 results")
         self.M, _, self.head_dim = (int(n) for n in self.x[0].shape)
+        _c_ints(**{"a size of x": max(int(n) for t in self.x for n in t.shape)})
         self.device, self.index, self.dtype = self.x[0].device, self.x[0].get_device(), self.x[0].dtype
         if out is None:
             out = [torch.empty(t.shape, dtype=out_dtype or self.dtype, device=self.device) for t in self.x]
