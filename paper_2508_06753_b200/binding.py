@@ -547,6 +547,8 @@ class Heads:
 
 def _rope_angles(heads: Heads, positions, inv_freq) -> int:
     """Checks positions and inv_freq; the number of values of a head that turn."""
+    if positions is None:
+        raise ValueError("positions are needed for the rotation")
     half, index = inv_freq.shape[0], heads.index
     if inv_freq.dtype is not _F64 or inv_freq.dim() != 1 or inv_freq.get_device() != index or not inv_freq.is_contiguous():
         _want(inv_freq, "inv_freq", _F64, (half,), heads.device)

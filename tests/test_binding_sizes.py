@@ -43,3 +43,13 @@ def test_frequencies(b):
         b.w2a8_rope_frequencies(64, 1e4, "llama3", factor=2.0, high=4.0, original_length=BIG + 8192, device="cpu")
     with pytest.raises(ValueError, match="32 bits"):
         b.w2a8_rope_frequencies(BIG + 64, 1e4, device="cpu")
+
+
+def test_rotation_without_positions(b, monkeypatch):
+    import torch
+    monkeypatch.setattr(b, "_launch_stream", lambda *a: 0)              # the checks behind the one for a device
+    heads, freq = b.Heads([torch.zeros((3, 2, 64))]), torch.zeros(32, dtype=torch.float64)
+    with pytest.raises(ValueError, match="positions"):
+        b.w2a8_qk_norm_rope(heads, 1e-6, inv_freq=freq)
+    with pytest.raises(ValueError, match="positions"):
+        b.w2a8_rope(heads, None, freq)
