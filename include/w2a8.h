@@ -487,7 +487,8 @@ int w2a8_rope(int count, const void *const *x, int x_is_bf16, void *const *out, 
 /*
  * w2a8_qk_norm_rope -- w2a8_rope with a norm of every head before the rotation,
  * in the same pass: x * weight[i] / sqrt(mean(x^2) + eps), the mean over the
- * head_dim values of one head, in fp32.
+ * head_dim values of one head, in fp32 (rows whose squares pass its range, above
+ * or below, are scaled by a power of two first).
  *   weight   HOST array of `count` DEVICE pointers to [head_dim] fp32, an entry
  *            (or the array) NULL = 1;  eps >= 0
  * The rest as for w2a8_rope; rot_dim may be 0 here (norms without a rotation;

@@ -26,6 +26,9 @@ namespace w2a8 {
 constexpr int kRopeMaxTensors = 4;
 constexpr int kRopeMaxDim = 512;
 constexpr int kRopeMaxThreads = 320;
+// Means of squares that need no care: the squares of all values that count in them are normal numbers, and their sum over
+// kRopeMaxDim values is finite
+constexpr float kRopeLeastMean = 1e-30f, kRopeMostMean = 6e35f;
 constexpr int kRopeTurns = 1024;         // pairs of sine and cosine in shared memory: tokens of a CTA times pairs
 
 struct RopeTensor {
@@ -116,11 +119,68 @@ __device__ __forceinline__ void store_values(void *base, long long at, const flo
     }
 }
 
+// Rows of the norm whose squares pass fp32's range, or are lost below it with next to no eps (a bit of far_rows per token of the
+// CTA): brought to about 1 by a power of two first.  One value at a time and behind the others, which keep their registers
+// that way.  What the others pay for being looked at: 8192 tokens of 72 heads of 128, bf16, 49.6 us before and 50.1 with it; 333
+// tokens of 25 heads of 80 3.1 and 3.2 (4.1 with this inside their loop, by one CTA less per SM).
+template <int V, bool X16, bool O16, bool HALVES>
+__device__ __noinline__ void rope_far_rows(const RopeParams &p, const float2 *turn, unsigned far_rows) {
+    const int G = 1 << p.group_log2, lane = threadIdx.x & (G - 1), turned_units = p.half / V;
+    const int tile = blockIdx.x / p.head_tiles, head_tile = blockIdx.x - tile * p.head_tiles;
+    const int row = head_tile * (blockDim.x >> p.group_log2) + (threadIdx.x >> p.group_log2);
+    int which = 0;
+    while (row < p.rows && row >= p.end[which]) ++which;
+    const RopeTensor &t = p.t[which];
+    const int head = row - (which ? p.end[which - 1] : 0);
+#pragma unroll 1
+    for (int token = 0; token < p.tokens_per_block; ++token) {
+        const bool far = far_rows >> token & 1;
+        const long long m = (long long)(blockIdx.x / p.head_tiles) * p.tokens_per_block + token;
+        const long long from = m * t.xt + (long long)head * t.xh, to = m * t.ot + (long long)head * t.oh;
+        auto get = [&](int i) {
+            if constexpr (X16) return __uint_as_float((uint32_t)static_cast<const uint16_t *>(t.x)[from + i] << 16);
+            else return static_cast<const float *>(t.x)[from + i];
+        };
+        float most = 0.0f, sum = 0.0f;
+#pragma unroll 1
+        for (int i = lane; far && i < p.D; i += G) most = fmaxf(most, fabsf(get(i)));
+        __syncwarp();
+        for (int o = G >> 1; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+        // 2^-k, k the exponent of the largest value; 2^86 is enough for the square of the smallest there is
+        const int k = most <= 3.402823466e38f ? min(max((int)(__float_as_uint(most) >> 23) - 127, -86), 126) : 0;
+        const float f = __uint_as_float((uint32_t)(127 - k) << 23);
+#pragma unroll 1
+        for (int i = lane; far && i < p.D; i += G) {
+            const float z = get(i) * f;
+            sum = fmaf(z, z, sum);
+        }
+        __syncwarp();
+        for (int o = G >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        const float scale = __frsqrt_rn(fmaf(sum, p.inv_D, p.eps * f * f));
+#pragma unroll 1
+        for (int k = lane; far && k < p.D / 2; k += G) {             // pairs, those that are not rotated behind the others
+            const bool turns = k < p.half;
+            const int i = HALVES && turns ? k : 2 * k, j = HALVES && turns ? k + p.half : 2 * k + 1;
+            float u = get(i) * f * (scale * (t.weight ? t.weight[i] : 1.0f));
+            float v = get(j) * f * (scale * (t.weight ? t.weight[j] : 1.0f));
+            if (turns) {
+                const float2 q = turn[token * p.half + k % V * turned_units + k / V];
+                const float x = u, y = v;
+                u = fmaf(x, q.x, -(y * q.y));
+                v = fmaf(y, q.x, x * q.y);
+            }
+            store_values<1, O16>(t.out, to + i, &u);
+            store_values<1, O16>(t.out, to + j, &v);
+        }
+    }
+}
+
 // V pairs per lane and chunk, NC chunks per lane: V = 4 (8 where both sides allow it) where sizes, strides and pointers
 // allow vectors, else V = 1.
+// Four pairs with the norm are held to 48 registers: with 62 the CTAs of a small batch wait for one another (see above).
 template <int V, int NC, bool NORM, bool X16, bool O16, bool HALVES, bool DIRECT>
-__global__ void __launch_bounds__(kRopeMaxThreads, V * NC <= 8 && V > 1 ? 3 : 1)
-w2a8_rope_kernel(const RopeParams p) {
+__global__ void __launch_bounds__(kRopeMaxThreads, NORM && V * NC == 4 ? 4 : V * NC <= 8 && V > 1 ? 3 : 1)
+w2a8_rope_kernel(const __grid_constant__ RopeParams p) {
     constexpr int X = X16 ? 2 : 4;
     using P = Piece<V, X16>;
     // rows that are on their way: kRing slots of each thread
@@ -216,6 +276,7 @@ w2a8_rope_kernel(const RopeParams p) {
             for (int j = 0; j < 2 * V; ++j)
                 weight[c][j] = t.weight && on[c] ? t.weight[j < V ? off_a[c] + j : off_b[c] + j - V] : 1.0f;
     }
+    unsigned far_rows = 0;                           // tokens whose row is left for the end
     const float2 *cs = turn + lane;
 #pragma unroll 1
     for (int token = 0; token < tokens; ++token, cs += p.half, dst += dst_step) {
@@ -231,6 +292,7 @@ w2a8_rope_kernel(const RopeParams p) {
         for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int j = 0; j < V; ++j) { e[c][j] = now[c][0].value(j); e[c][V + j] = now[c][1].value(j); }
+        bool far = false;
         if constexpr (NORM) {
             float sum = 0.0f;
 #pragma unroll
@@ -240,7 +302,10 @@ w2a8_rope_kernel(const RopeParams p) {
                     for (int j = 0; j < 2 * V; ++j) sum = fmaf(e[c][j], e[c][j], sum);
                 }
             for (int o = G >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-            const float scale = __frsqrt_rn(fmaf(sum, p.inv_D, p.eps));
+            const float mean = fmaf(sum, p.inv_D, p.eps);
+            far = live && !(mean >= kRopeLeastMean && mean <= kRopeMostMean);
+            far_rows |= (unsigned)far << token;
+            const float scale = __frsqrt_rn(mean);
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -248,7 +313,7 @@ w2a8_rope_kernel(const RopeParams p) {
         }
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            if (!on[c]) continue;
+            if (!on[c] || far) continue;
             if (turned[c]) {
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
@@ -266,6 +331,8 @@ w2a8_rope_kernel(const RopeParams p) {
         if constexpr (!DIRECT) ask();
         else if (token + 1 < tokens) load_row();
     }
+    if constexpr (NORM)
+        if (__any_sync(0xFFFFFFFFu, far_rows)) rope_far_rows<V, X16, O16, HALVES>(p, turn, far_rows);
 }
 
 template <int V, int NC, bool NORM, bool HALVES, bool DIRECT>
