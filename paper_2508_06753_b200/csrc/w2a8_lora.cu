@@ -610,6 +610,7 @@ w2a8_lora_kernel(const LoraParams p) {
             // The results of a block that are NaN, again: from s h in fp32 and what the stage still holds of B and base.  The
             // others keep their bits, so an infinite weight touches its channel alone.
             auto again = [&](uint32_t st, int blk) {
+                asm volatile("" ::: "memory");                        // reads what `block` stored as another type
 #pragma unroll 1
                 for (int v = 0; v < 8; ++v) {
                     const int row = v < 4 ? ra : rb, ch = blk * 16 + 4 * t + (v & 3);
