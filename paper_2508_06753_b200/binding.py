@@ -116,6 +116,19 @@ def _ptr(t) -> int:
     return 0 if t is None else int(t.data_ptr())
 
 
+def _new(shape, dtype, device, stream=None) -> torch.Tensor:
+    """A result's memory for a launch on `stream`: of that stream, since what the current one frees may still be written
+    by its earlier work, and kept for the current one, where the result is read."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    here = torch.cuda.current_stream(device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if here != stream:
+        t.record_stream(here)
+    return t
+
+
 def w2a8_version() -> int:
     return int(lib().w2a8_version())
 
@@ -134,7 +147,7 @@ def w2a8_linear_host_workspace_bytes(M: int, N: int, K: int, group: int) -> int:
 
 def new_workspace(nbytes: int, device="cuda", stream=None) -> torch.Tensor:
     """Allocate and zero-fill a workspace of at least `nbytes` bytes."""
-    ws = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+    ws = _new(max(int(nbytes), 256), torch.uint8, device, stream)
     w2a8_workspace_init(ws, stream)
     return ws
 
@@ -153,7 +166,7 @@ def w2_pack(codes: torch.Tensor, packed: torch.Tensor | None = None, stream=None
     """codes uint8 [N][K] (device) -> packed int32 [N][K/16] (bit pattern of uint32)."""
     N, K = codes.shape
     if packed is None:
-        packed = torch.empty((N, max(K // 16, 1)), dtype=torch.int32, device=codes.device)
+        packed = _new((N, max(K // 16, 1)), torch.int32, codes.device, stream)
     _check(lib().w2_pack(_ptr(codes), N, K, _ptr(packed), _stream(stream)), "w2_pack")
     return packed
 
@@ -163,9 +176,9 @@ def a8_quantize(x_bf16: torch.Tensor, a: torch.Tensor | None = None,
     """x bf16 [M][K] (device) -> (a int8 [M][K], a_scale fp32 [M])."""
     M, K = x_bf16.shape
     if a is None:
-        a = torch.empty((M, K), dtype=torch.int8, device=x_bf16.device)
+        a = _new((M, K), torch.int8, x_bf16.device, stream)
     if a_scale is None:
-        a_scale = torch.empty((M,), dtype=torch.float32, device=x_bf16.device)
+        a_scale = _new((M,), torch.float32, x_bf16.device, stream)
     _check(lib().a8_quantize(_ptr(x_bf16), M, K, _ptr(a), _ptr(a_scale), _stream(stream)),
            "a8_quantize")
     return a, a_scale
@@ -177,7 +190,7 @@ def w2a8_gemm(a: torch.Tensor, a_scale: torch.Tensor, packed: torch.Tensor, w_sc
     M, K = a.shape
     N = packed.shape[0]
     if y is None:
-        y = torch.empty((M, N), dtype=torch.float32, device=a.device)
+        y = _new((M, N), torch.float32, a.device, stream)
     _check(lib().w2a8_gemm(_ptr(a), _ptr(a_scale), _ptr(packed), _ptr(w_scale), _ptr(y), M, N, K,
                            group, _ptr(workspace), workspace.numel() * workspace.element_size(),
                            _stream(stream)), "w2a8_gemm")
@@ -230,7 +243,7 @@ def w2a8_gemm_h16(a: torch.Tensor, a_scale: torch.Tensor, packed: torch.Tensor, 
     if w_scale_h.dtype != torch.float16:
         raise TypeError("w_scale_h must be float16")
     if y is None:
-        y = torch.empty((M, N), dtype=out_dtype, device=a.device)
+        y = _new((M, N), out_dtype, a.device, stream)
     if y.dtype not in (torch.float32, torch.bfloat16):
         raise TypeError("y must be float32 or bfloat16")
     _check(lib().w2a8_gemm_h16(_ptr(a), _ptr(a_scale), _ptr(packed), _ptr(w_scale_h), _ptr(y),
@@ -248,7 +261,7 @@ def w2a16_gemm(x: torch.Tensor, packed: torch.Tensor, w_scale: torch.Tensor, gro
     if x.dtype != torch.bfloat16:
         raise TypeError("x must be bfloat16")
     if y is None:
-        y = torch.empty((M, N), dtype=torch.float32, device=x.device)
+        y = _new((M, N), torch.float32, x.device, stream)
     _check(lib().w2a16_gemm(_ptr(x), _ptr(packed), _ptr(w_scale), _ptr(y), M, N, K, group, _ptr(workspace),
                             workspace.numel() * workspace.element_size(), _stream(stream)), "w2a16_gemm")
     return y
@@ -262,11 +275,11 @@ def w2a8_linear(x: torch.Tensor, packed: torch.Tensor, w_scale: torch.Tensor, gr
     M, K = x.shape
     N = packed.shape[0]
     if a is None:
-        a = torch.empty((M, K), dtype=torch.int8, device=x.device)
+        a = _new((M, K), torch.int8, x.device, stream)
     if a_scale is None:
-        a_scale = torch.empty((M,), dtype=torch.float32, device=x.device)
+        a_scale = _new((M,), torch.float32, x.device, stream)
     if y is None:
-        y = torch.empty((M, N), dtype=torch.float32, device=x.device)
+        y = _new((M, N), torch.float32, x.device, stream)
     _check(lib().w2a8_linear(_ptr(x), _ptr(a), _ptr(a_scale), _ptr(packed), _ptr(w_scale), _ptr(y), M, N, K,
                              group, _ptr(workspace), workspace.numel() * workspace.element_size(),
                              _stream(stream)), "w2a8_linear")
@@ -279,7 +292,7 @@ def w2a8_gemm_partials(a: torch.Tensor, packed: torch.Tensor, group: int, worksp
     M, K = a.shape
     N = packed.shape[0]
     if partials is None:
-        partials = torch.empty((M, N, K // group), dtype=torch.int32, device=a.device)
+        partials = _new((M, N, K // group), torch.int32, a.device, stream)
     _check(lib().w2a8_gemm_partials(_ptr(a), _ptr(packed), _ptr(partials), M, N, K, group,
                                     _ptr(workspace), workspace.numel() * workspace.element_size(),
                                     _stream(stream)), "w2a8_gemm_partials")
@@ -343,7 +356,7 @@ def w2a8_gemm_grouped(a: torch.Tensor, a_scale: torch.Tensor, grp: Group, group:
     if y is not None:
         grp.bind_outputs(y)
     elif grp.y is None or grp.y[0].shape[0] != M:
-        grp.bind_outputs([torch.empty((M, n), dtype=torch.float32, device=a.device) for n in grp.N])
+        grp.bind_outputs([_new((M, n), torch.float32, a.device, stream) for n in grp.N])
     _check(lib().w2a8_gemm_grouped(_ptr(a), _ptr(a_scale), grp.count, grp._pk, grp._sc, grp._y, grp._n, M, K,
                                    group, _ptr(workspace), workspace.numel() * workspace.element_size(),
                                    _stream(stream)), "w2a8_gemm_grouped")
@@ -358,7 +371,7 @@ def w2a8_linear_grouped(x: torch.Tensor, grp: Group, group: int, workspace: torc
     if y is not None:
         grp.bind_outputs(y)
     elif grp.y is None or grp.y[0].shape[0] != M:
-        grp.bind_outputs([torch.empty((M, n), dtype=torch.float32, device=x.device) for n in grp.N])
+        grp.bind_outputs([_new((M, n), torch.float32, x.device, stream) for n in grp.N])
     _check(lib().w2a8_linear_grouped(_ptr(x), _ptr(a), _ptr(a_scale), grp.count, grp._pk, grp._sc, grp._y,
                                      grp._n, M, K, group, fuse, _ptr(workspace),
                                      workspace.numel() * workspace.element_size(), _stream(stream)),
@@ -471,7 +484,7 @@ def w2a8_lora_grouped(x: torch.Tensor, adapter: torch.Tensor, lora: LoraGroup, b
     if dtype is not _F32 and dtype is not _BF16:
         raise TypeError("base and y must be float32 or bfloat16")
     if y is None:
-        y = [torch.empty((M, n), dtype=dtype, device=device) for n in lora.N]
+        y = [_new((M, n), dtype, device, stream) for n in lora.N]
     py = lora._outputs("y", y, M, dtype, index)
     pb = None if base is None else py if base is y else lora._outputs("base", base, M, dtype, index)
     status = lib().w2a8_lora_grouped(x.data_ptr(), adapter.data_ptr(), lora.adapters, lora.rank_max, lora._rank,
@@ -607,7 +620,7 @@ def w2a8_gemm_static(a: torch.Tensor, a_scale: torch.Tensor, packed: torch.Tenso
     M, K = a.shape
     N = packed.shape[0]
     if y is None:
-        y = torch.empty((M, N), dtype=torch.float32, device=a.device)
+        y = _new((M, N), torch.float32, a.device, stream)
     _check(lib().w2a8_gemm_static(_ptr(a), _ptr(a_scale), _ptr(packed), _ptr(w_scale), _ptr(y), M, N, K,
                                   group, _stream(stream)), "w2a8_gemm_static")
     return y
