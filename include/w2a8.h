@@ -477,8 +477,10 @@ int w2a8_rope_frequencies(int rot_dim, double base, int scaling, double factor, 
  *                overlap.  Elements between the rows are neither read nor written.
  *   positions    [M] int32;  inv_freq  [rot_dim / 2] double (8-byte alignment)
  * M up to 2^30; head_dim even, 2 .. 512; rot_dim even, 2 .. head_dim; at most
- * 2^17 heads in all.  Head sizes, rot_dim and
- * strides that are multiples of 8 take 16-byte accesses.
+ * 2^17 heads in all.  Where head_dim, rot_dim and all strides are multiples of 8,
+ * fp32 rows take 16-byte accesses and bf16 rows 8-byte ones (16-byte ones where
+ * head_dim and rot_dim are multiples of 16); else values go one by one, at about a
+ * tenth of the rate.
  */
 int w2a8_rope(int count, const void *const *x, int x_is_bf16, void *const *out, int out_is_bf16, const int *heads,
               const int64_t *x_strides, const int64_t *out_strides, int M, int head_dim, int rot_dim, int interleaved,

@@ -517,7 +517,8 @@ class Heads:
     """Host-side argument block of the rope entry points: results x[i] [M][heads_i][head_dim] (fp32, or all bf16;
     views with strides are fine as long as the values of a head are consecutive), the outputs, and the norms' weights
     (fp32 [head_dim] or None, one per result).  out: a list of the same shapes (fp32 or bf16), `x` itself for in
-    place, or None: new ones of out_dtype (None: x's).  Built once and reused every call."""
+    place, or None: new ones of out_dtype (None: x's), memory of the current stream.  Built once and reused every
+    call."""
 
     def __init__(self, x, out=None, weight=None, out_dtype=None):
         self.x = list(x)

@@ -24,10 +24,11 @@
 // The products are mma.sync (8 clk per m16n8k16 and scheduler): an item's accumulators have 16 to 128 columns in step 1
 // and 16 rows per warp in step 2, and both have to leave the tensor core's sum early, for its truncation.  What bounds the
 // kernel (device time, calls over inputs larger than L2): gate|up of the 8B layer for 8192 tokens of 16 adapters of rank 64,
-// 400 us, 5.0 TB/s of the 2.02 GB it cannot do without; about 30 us of an item's 200 are step 1, when the memory idles,
-// and in step 2 the issue of two warps per scheduler (0.32 a clock; tensor pipe 36 %).  32 tokens with an adapter each 38 us,
-// 2.5 TB/s: the same issue, with 15 of 16 rows of an instruction empty.  One token, q|k|v: 6.5 us of latencies: owners, sort,
-// addresses, first bytes, two cluster barriers.
+// 398 us for three calls in a row, 5.1 TB/s of the 2.02 GB it cannot do without, and 450 us for sixty, when the power limit
+// takes the clock from 1965 to 1700 MHz; about 30 us of an item's 200 are step 1, when the memory idles, and in step 2 the
+// issue of two warps per scheduler (0.34 a clock, tensor pipe 37 %: counters of 1024 tokens of 2 adapters).  32 tokens with
+// an adapter each 38 us, 2.4 TB/s: the same issue, with 15 of 16 rows of an instruction empty.  One token, q|k|v: 6.5 us of
+// latencies: owners, sort, addresses, first bytes, two cluster barriers.
 #include "w2a8_common.cuh"
 
 namespace w2a8 {
@@ -685,8 +686,9 @@ static cudaError_t launch_lora(LoraParams &p, cudaStream_t st) {
     // The cluster size by the estimate above, for a guess of the tiles.  Decode batches: one per adapter that there is a token
     // for.  Many tokens: the full ones and one more per adapter, but no more of these than of the full ones and two (resident
     // adapters need not be in use: 600 tokens of 6 of 60 adapters of rank 16, 4096 x 4096, take 18.8 us with the clusters of
-    // two that 60 tiles ask for, 15.8 with the four of this guess).  The number of clusters is for as many tiles as there may
-    // be (tokens without an adapter can be one more).
+    // two that 60 tiles ask for, 15.8 with the four of this guess).  The number of clusters is for as many tiles as all tokens
+    // may be in one sort (those without an adapter can be one more); where the chunks of 256 tokens of 16-token instances make
+    // more, the clusters take them in turn.
     const int used = p.M < p.adapters ? p.M : p.adapters, full = p.M / T, bound = full + used + 1;
     const int more = used < full + 2 ? used : full + 2;
     const int tiles = T == 16 && p.M <= (long long)used * T ? used : p.M < (1 << 24) ? full + more : (1 << 24) / T;
@@ -719,7 +721,8 @@ static cudaError_t launch_lora_rank(LoraParams &p, bool y16, cudaStream_t st) {
     // Tiles of 16 tokens for decode batches: few tokens, or many adapters for the tokens.  Tiles of 16 / 64, us: 256 tokens of
     // 64 adapters of rank 64, gate|up of the 8B layer, 68 / 209, 300 tokens 90 / 185; 256 tokens of one adapter 27 / 29; 1024
     // tokens of 4 adapters of rank 32 73 / 62; 500 tokens, q|k|v, rank 32, 64 resident adapters: 64 in use 36 / 72, 5 in use
-    // 31 / 22.
+    // 31 / 22.  The host knows the adapters that are resident, not those in use, and pays where these are few: q|k|v, rank 16,
+    // 2048 tokens of 5 of 256 adapters 79 / 40, 8192 tokens of 64 of 1024 290 / 176, of one of 1024 343 / 143.
     const int tile = env_int("W2A8_LORA_TILE", p.M <= 256 || p.M <= 8 * p.adapters ? 16 : 64);
     if (tile == 16) return y16 ? launch_lora<16, RK, true>(p, st) : launch_lora<16, RK, false>(p, st);
     return y16 ? launch_lora<64, RK, true>(p, st) : launch_lora<64, RK, false>(p, st);
